@@ -415,7 +415,8 @@ rago_status rago_q4_rescore_backward(const uint8_t* codes, const void* scales, r
  *   out_stats   dev fp32 [nq][RAGO_POLICY_STATS], 16-byte aligned: the rows' maxima and sums, for the backward pass
  * A query without candidates has policy = kl = 0.  Scores may be of any size, the type's lowest value as a mask among them; where
  * log rho is -infinity or beyond the range of fp32 and pi > 0, kl is infinite or beyond it, as the formula says, and that query's gradient
- * NaN or infinite.  A NaN or +infinity among the candidates makes that query's results NaN, and no other's.
+ * NaN or infinite.  (exp(x) below 2^-126 of the row's largest is 0, and so is pi then, wherever the candidate stands.)  A NaN or
+ * +infinity among the candidates makes that query's results NaN, and no other's.
  *   workspace   dev, 256-byte aligned, rago_policy_workspace_bytes(...) bytes: the partial sums of long rows (0 bytes, and then
  *               NULL will do, for rows of up to 16 384 candidates).  Two calls that overlap on the GPU need distinct ones
  * C >= 1, nq * C < 2^40, 0 <= G <= 1024.  Sums are fp32, in a fixed order.

@@ -43,8 +43,11 @@ __device__ __forceinline__ float load_s(const void* base, size_t i) {
 // Running sums of one row, relative to m (policy) and mr (reference), base 2; m and mr are unit * score.  The sums of policy and
 // reference go through the same roundings (spelled out: contracted differently they would differ), so equal scores give kl = 0
 // exactly.
-struct PolicySums { float m, Z, mr, Zr, E; };  // E = sum 2^t unit * (score - ref)
-__device__ __forceinline__ PolicySums policy_none() { return {RAGO_NEG_INF, 0.f, RAGO_NEG_INF, 0.f, 0.f}; }
+// A candidate that the reference has at -infinity makes kl infinite if pi > 0 and adds nothing if pi = 0.  Which of the two it is shows
+// against the row's best score only, not against the best so far, so such a candidate stays out of E (infinity times a weight that
+// shrinks to 0 later would be NaN): the best of them is kept, and looked at in the end.
+struct PolicySums { float m, Z, mr, Zr, E, lost; };  // E = sum 2^t unit * (score - ref), lost = the best unit * score with ref = -infinity
+__device__ __forceinline__ PolicySums policy_none() { return {RAGO_NEG_INF, 0.f, RAGO_NEG_INF, 0.f, 0.f, RAGO_NEG_INF}; }
 
 // 2^x as one instruction (2 units in the last place; below 2^-126 zero, which is what such a weight adds)
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -56,10 +59,15 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 2^((from - to) step), where both may be -infinity
 __device__ __forceinline__ float policy_rescale(float from, float to, float step) { return from == to ? 1.f : exp2_fast((from - to) * step); }
 
-// Adds n candidates (bit i of `missing`: not there).  A missing candidate takes the score -infinity: its weight is 0 like anything
+__device__ __forceinline__ bool policy_there(const PolicyArgs& A, size_t at, float score) {
+    return (A.ids == nullptr || A.ids[at] >= 0) && score != A.lowest;
+}
+
+// Adds n candidates, number `at` on (bit i of `missing`: not there).  A missing candidate takes the score -infinity: its weight is 0 like anything
 // else's, and so no candidate needs a branch.  The maxima move at most once for all of them.
-template <int n, bool REF, bool IDS>
-__device__ __forceinline__ void policy_add(PolicySums& S, float (&score)[n], float (&ref)[n], uint32_t missing, float step, float unit) {
+template <int n, bool BF16, bool REF, bool IDS>
+__device__ __forceinline__ void policy_add(const PolicyArgs& A, size_t at, PolicySums& S, float (&score)[n], float (&ref)[n], uint32_t missing) {
+    const float step = A.step, unit = A.unit;
     float top = RAGO_NEG_INF, top_r = RAGO_NEG_INF;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
@@ -83,6 +91,7 @@ __device__ __forceinline__ void policy_add(PolicySums& S, float (&score)[n], flo
         if (top_r > S.mr) { S.Zr = __fmul_rn(S.Zr, exp2_fast((S.mr - top_r) * step)); S.mr = top_r; }
         mr = S.mr == RAGO_NEG_INF ? 0.f : S.mr;
     }
+    const float E = S.E;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
         const float w = exp2_fast((score[i] - m) * step);
@@ -92,23 +101,40 @@ __device__ __forceinline__ void policy_add(PolicySums& S, float (&score)[n], flo
             if (!(w == 0.f)) S.E = fmaf(w, score[i] - ref[i], S.E);
         }
     }
+    if (REF && S.E == __int_as_float(0x7f800000)) {  // once more, without the references at -infinity, and from memory: nothing stays in registers for it
+        S.E = E;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const float raw = load_s<BF16>(A.scores, at + i), r = load_s<BF16>(A.ref, at + i) * unit, s = policy_there(A, at + i, raw) ? raw * unit : RAGO_NEG_INF;
+            const float w = exp2_fast((s - m) * step);
+            if (w == 0.f) continue;
+            if (r == RAGO_NEG_INF) S.lost = fmaxf(S.lost, s);
+            else S.E = fmaf(w, s - r, S.E);
+        }
+    }
 }
+template <bool REF>
 __device__ __forceinline__ void policy_join(PolicySums& S, const PolicySums& o, float step) {
     const float m = fmaxf(S.m, o.m), f = policy_rescale(S.m, m, step), g = policy_rescale(o.m, m, step);
     S.Z = fmaf(S.Z, f, __fmul_rn(o.Z, g));
-    S.E = fmaf(S.E, f, __fmul_rn(o.E, g));
     S.m = m;
+    if (!REF) return;
+    S.E = fmaf(S.E, f, __fmul_rn(o.E, g));
     const float mr = fmaxf(S.mr, o.mr);
     S.Zr = fmaf(S.Zr, policy_rescale(S.mr, mr, step), __fmul_rn(o.Zr, policy_rescale(o.mr, mr, step)));
     S.mr = mr;
+    S.lost = fmaxf(S.lost, o.lost);
 }
+template <bool REF>
 __device__ __forceinline__ PolicySums policy_shfl(const PolicySums& S, int o) {
-    PolicySums r;
+    PolicySums r = policy_none();
     r.m = __shfl_xor_sync(0xffffffffu, S.m, o);
     r.Z = __shfl_xor_sync(0xffffffffu, S.Z, o);
+    if (!REF) return r;
     r.mr = __shfl_xor_sync(0xffffffffu, S.mr, o);
     r.Zr = __shfl_xor_sync(0xffffffffu, S.Zr, o);
     r.E = __shfl_xor_sync(0xffffffffu, S.E, o);
+    r.lost = __shfl_xor_sync(0xffffffffu, S.lost, o);
     return r;
 }
 
@@ -126,11 +152,8 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicySums& S, bool has_re
 }
 // the logarithm of the quotient, not the difference of the logarithms: near policies have near sums
 __device__ __forceinline__ float policy_kl(const PolicyArgs& A, const PolicySums& S) {
-    return fmaf(S.E / S.Z - (S.m - (S.mr == RAGO_NEG_INF ? 0.f : S.mr)), A.scale / A.unit, LN2 * log2f(S.Zr / S.Z));
-}
-
-__device__ __forceinline__ bool policy_there(const PolicyArgs& A, size_t at, float score) {
-    return (A.ids == nullptr || A.ids[at] >= 0) && score != A.lowest;
+    const float E = S.lost > RAGO_NEG_INF && exp2_fast((S.lost - S.m) * A.step) != 0.f ? __int_as_float(0x7f800000) : S.E;
+    return fmaf(E / S.Z - (S.m - (S.mr == RAGO_NEG_INF ? 0.f : S.mr)), A.scale / A.unit, LN2 * log2f(S.Zr / S.Z));
 }
 
 // log pi of sample t of row q and whether it counts
@@ -226,21 +249,21 @@ __device__ __forceinline__ void policy_sweep(const PolicyArgs& A, int q, int beg
         P::load(A.scores, next, true, s[1]);
         if (REF) { P::load(A.ref, at, ref_whole, r[0]); P::load(A.ref, next, ref_whole, r[1]); }
         const uint32_t m0 = IDS ? policy_missing<P::UNIT>(A.ids, at) : 0u, m1 = IDS ? policy_missing<P::UNIT>(A.ids, next) : 0u;
-        policy_add<P::UNIT, REF, IDS>(S, s[0], r[0], m0, A.step, A.unit);
-        policy_add<P::UNIT, REF, IDS>(S, s[1], r[1], m1, A.step, A.unit);
+        policy_add<P::UNIT, BF16, REF, IDS>(A, at, S, s[0], r[0], m0);
+        policy_add<P::UNIT, BF16, REF, IDS>(A, next, S, s[1], r[1], m1);
     }
     if (p < pieces) {
         const size_t at = row + head + (size_t)p * P::UNIT;
         float s[P::UNIT], r[P::UNIT];
         P::load(A.scores, at, true, s);
         if (REF) P::load(A.ref, at, ref_whole, r);
-        policy_add<P::UNIT, REF, IDS>(S, s, r, IDS ? policy_missing<P::UNIT>(A.ids, at) : 0u, A.step, A.unit);
+        policy_add<P::UNIT, BF16, REF, IDS>(A, at, S, s, r, IDS ? policy_missing<P::UNIT>(A.ids, at) : 0u);
     }
     // the numbers in front and behind, less than a piece each
     for (int i = first; i < head + n - tail; i += stride) {
         const size_t at = row + (i < head ? i : tail + i - head);
         float s[1] = {load_s<BF16>(A.scores, at)}, r[1] = {REF ? load_s<BF16>(A.ref, at) : 0.f};
-        policy_add<1, REF, IDS>(S, s, r, IDS ? policy_missing<1>(A.ids, at) : 0u, A.step, A.unit);
+        policy_add<1, BF16, REF, IDS>(A, at, S, s, r, IDS ? policy_missing<1>(A.ids, at) : 0u);
     }
 }
 
@@ -255,7 +278,7 @@ __global__ void __launch_bounds__(POLICY_WARPS * 32) policy_forward_short_kernel
     if (q >= A.nq) return;
     PolicySums S = policy_none();
     policy_sweep<BF16, REF, IDS>(A, q, 0, A.C, lane, 32, S);
-    for (int o = 16; o; o >>= 1) policy_join(S, policy_shfl(S, o), A.step);
+    for (int o = 16; o; o >>= 1) policy_join<REF>(S, policy_shfl<REF>(S, o), A.step);
     bool none;
     const PolicyRow r = policy_row(S, REF, A.unit, &none);
     float sum = 0.f;
@@ -303,13 +326,14 @@ __device__ __forceinline__ void policy_finish(const PolicyArgs& A, int q, Policy
 }
 
 // The threads' sums, joined; the same in every thread
+template <bool REF>
 __device__ __forceinline__ PolicySums policy_join_block(const PolicyArgs& A, PolicySums S, PolicySums* part) {
-    for (int o = 16; o; o >>= 1) policy_join(S, policy_shfl(S, o), A.step);
+    for (int o = 16; o; o >>= 1) policy_join<REF>(S, policy_shfl<REF>(S, o), A.step);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = S;
     __syncthreads();
     S = part[0];
 #pragma unroll
-    for (int w = 1; w < POLICY_THREADS / 32; ++w) policy_join(S, part[w], A.step);
+    for (int w = 1; w < POLICY_THREADS / 32; ++w) policy_join<REF>(S, part[w], A.step);
     return S;
 }
 
@@ -323,7 +347,7 @@ __global__ void __launch_bounds__(POLICY_THREADS) policy_forward_long_kernel(con
     const int q = blockIdx.x / spans, begin = blockIdx.x % spans * POLICY_SPAN;
     PolicySums S = policy_none();
     policy_sweep<BF16, REF, IDS>(A, q, begin, min(A.C - begin, POLICY_SPAN), threadIdx.x, POLICY_THREADS, S);
-    S = policy_join_block(A, S, part);
+    S = policy_join_block<REF>(A, S, part);
     if (spans > 1) {
         if (threadIdx.x == 0) sums[blockIdx.x] = S;
     } else {
@@ -339,8 +363,8 @@ __global__ void __launch_bounds__(POLICY_THREADS) policy_finish_kernel(const Pol
     grid_dependency_wait();
     grid_dependents_may_launch();
     PolicySums S = policy_none();
-    for (int i = threadIdx.x; i < spans; i += POLICY_THREADS) policy_join(S, sums[(size_t)blockIdx.x * spans + i], A.step);
-    policy_finish<BF16, REF>(A, blockIdx.x, policy_join_block(A, S, part), terms, out_policy, out_kl, out_logp, out_stats);
+    for (int i = threadIdx.x; i < spans; i += POLICY_THREADS) policy_join<REF>(S, sums[(size_t)blockIdx.x * spans + i], A.step);
+    policy_finish<BF16, REF>(A, blockIdx.x, policy_join_block<REF>(A, S, part), terms, out_policy, out_kl, out_logp, out_stats);
 }
 
 // ---- backward --------------------------------------------------------------------------------------------------------------
