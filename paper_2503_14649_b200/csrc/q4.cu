@@ -90,8 +90,8 @@ __device__ __forceinline__ void q4_pairs(uint32_t word, const Q4Consts& K, uint3
     v[0] = low_pair(word); v[1] = high_pair(word); v[2] = low_pair(high); v[3] = high_pair(high);
 }
 
-// Powers of two that bring the queries' largest numbers to 2^14 .. 2^15, and their reciprocals; 1 for a query that is zero or
-// not finite.  A warp per query.
+// Powers of two that bring the queries' largest numbers to 2^14 .. 2^15, and their reciprocals; 1 for a query that is zero; 1 and infinity
+// for one that is not finite, whose results are all infinite or NaN.  A warp per query.
 template <bool QBF16>
 __device__ __forceinline__ void q4_query_units(float* __restrict__ unit, float* __restrict__ back, const void* __restrict__ queries, int q0, int nq, int d) {
     for (int q = threadIdx.x >> 5; q < nq; q += blockDim.x >> 5) {
@@ -115,7 +115,7 @@ __device__ __forceinline__ void q4_query_units(float* __restrict__ unit, float* 
         k = k > 126 ? 126 : k;
         if ((threadIdx.x & 31) == 0) {
             unit[q] = __uint_as_float((uint32_t)(127 + k) << 23);
-            back[q] = __uint_as_float((uint32_t)(127 - k) << 23);
+            back[q] = e == 255 ? __int_as_float(0x7f800000) : __uint_as_float((uint32_t)(127 - k) << 23);
         }
     }
 }
@@ -175,10 +175,46 @@ __device__ __forceinline__ uint4 q4_lds4(uint32_t addr) {
     return v;
 }
 
+// <query, row> as it stands, by one thread: the sum over a group, then its scale.  `x` is the query, fp32 or bf16.
+template <bool QBF16, bool SBF16>
+__device__ __forceinline__ float q4_score_direct(const uint8_t* __restrict__ codes, const void* __restrict__ scales, const void* __restrict__ x, int d, int group) {
+    float total = 0.f;
+    for (int i0 = 0; i0 < d; i0 += group) {
+        float sum = 0.f;
+        const int i1 = min(d, i0 + group);
+        for (int i = i0; i < i1; ++i) sum = fmaf(load_f<QBF16>(x, i), (float)((codes[i >> 1] >> (4 * (i & 1))) & 15) - 8.f, sum);
+        total = fmaf(load_f<SBF16>(scales, i0 / group), sum, total);
+    }
+    return total;
+}
+
+// The unit comes off last, so a total may leave the range of fp32 where the score, up to 2^140 times smaller, does not (a short query,
+// large scales).  A warp that has met one looks the results of its tiles through and takes what is not finite again without a unit, number by
+// number: rare, and right for all that fp32 holds.  A function of its own, called behind the last tile, and the rows' description left
+// in the kernel's parameters: inlined, or with a copy of them on the stack, it cost the loop 3 to 8% (registers).
+template <int MODE, bool SBF16, int NT>
+__device__ __noinline__ void q4_scores_again(const Q4Rows& R, const void* __restrict__ queries, int q0, int nq, int split, const float* back, float* __restrict__ out) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, teams = (blockDim.x >> 5) / split;
+    const int tiles = (int)((R.N + Q4S_ROWS - 1) / Q4S_ROWS), step = gridDim.x * teams;
+    constexpr bool QB = MODE == Q4_BF16;
+    for (int tile = warp / split * gridDim.x + blockIdx.x; tile < tiles; tile += step) {
+        const int64_t last = R.N > Q4S_ROWS ? R.N - Q4S_ROWS : 0, top = (int64_t)tile * Q4S_ROWS < last ? (int64_t)tile * Q4S_ROWS : last;
+#pragma unroll 1
+        for (int i = 0; i < NT * 8; ++i) {
+            const int q = (i >> 3) * 8 + 2 * t + (i & 1), r = g + 8 * ((i >> 1) & 3);
+            if (q >= nq || (MODE == Q4_F32_PACKED && t >= 2) || r >= R.N || !(back[q] < __int_as_float(0x7f800000))) continue;
+            float* const at = out + (size_t)(q0 + q) * R.N + top + r;
+            if (fabsf(*at) < __int_as_float(0x7f800000)) continue;
+            *at = q4_score_direct<QB, SBF16>(R.codes + (size_t)(top + r) * (R.d / 2), static_cast<const uint8_t*>(R.scales) + (size_t)(top + r) * R.groups * (SBF16 ? 2 : 4),
+                                             static_cast<const uint8_t*>(queries) + (size_t)(q0 + q) * R.d * (QB ? 2 : 4), R.d, R.group);
+        }
+    }
+}
+
 // SBF16: scales in bf16; GB = group / 32; NT tiles of 8 queries; STAGES of a warp's ring.  `split` warps share the chunks of a tile
 // (1 unless there are few rows): each sums its own part, the first adds the others' up.
 template <int MODE, bool SBF16, int GB, int NT, int WARPS, int STAGES, bool SPLIT>
-__global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 2 : 1) q4_scores_kernel(const Q4Rows R, const void* __restrict__ queries, int q0, int nq, int shared_by,
+__global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 2 : 1) q4_scores_kernel(const __grid_constant__ Q4Rows R, const void* __restrict__ queries, int q0, int nq, int shared_by,
                                                                float* __restrict__ out) {
     const int split = SPLIT ? shared_by : 1;
     constexpr int PARTS = MODE == Q4_F32 ? 2 : 1, ES = SBF16 ? 2 : 4;
@@ -259,6 +295,7 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 2 : 1) q4_scores_kern
     const Q4Consts K = q4_consts(nq);
     uint32_t slot = ring + t * 4;
     const uint32_t slot_end = slot + STAGES * Q4S_STAGE;
+    float finite = 0.f;  // NaN once a total is not
     for (int tile = first; tile < tiles; tile += step) {
         float total[2][NT][4] = {};
         uint32_t x = xs;
@@ -355,11 +392,13 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 2 : 1) q4_scores_kern
                     float v = total[r / 2][n][2 * (r & 1) + c];
                     // column 4 p + q holds part p: threads t and t + 2 hold the two parts of a query
                     if (MODE == Q4_F32_PACKED) v += __shfl_xor_sync(0xffffffffu, v, 2);
+                    finite = fmaf(v, 0.f, finite);
                     if (writes && g + 8 * r < R.N) __stcs(dst + row_of[r], v * u);
                 }
             }
     }
     cp_async_wait<0>();
+    if (!(finite == 0.f) && member == 0) q4_scores_again<MODE, SBF16, NT>(R, queries, q0, nq, split, back, out);
 }
 
 // ---- candidates -----------------------------------------------------------------------------------------------------------

@@ -88,6 +88,33 @@ def test_scores_hold_queries_of_any_size():
     check_scores(codes, scales, q, 64)
 
 
+@pytest.mark.parametrize("nq,query", [(1, "f32"), (4, "f32"), (20, "f32"), (3, "bf16"), (40, "bf16")])
+@pytest.mark.parametrize("scale,group", [("f32", 32), ("bf16", 128)])
+def test_scores_hold_scales_of_any_size(nq, query, scale, group):
+    """Scales up to 2e32 with queries around 1e-28 and around 1: every score, up to 1e35, is a number that fp32 holds."""
+    for N in (5, 300, 20_001):
+        codes, scales = make_rows(N, 256, group, DTYPES[scale])
+        q = make_queries(nq, 256, torch.float32)
+        scales[::3] *= 1e34
+        q[::2] *= 1e-28
+        check_scores(codes, scales, q.to(DTYPES[query]), group)
+
+
+def test_scores_beyond_fp32_are_infinite_and_no_others():
+    codes, scales = make_rows(100, 128, 64, torch.float32)
+    codes[7] = 0x99                                     # ones
+    scales[7] = 1e37
+    q = make_queries(9, 128, torch.float32)
+    q[1] = 1.0
+    q[2] = -1.0
+    got = binding.rago_q4_scores(codes, scales, q, 64)
+    assert got[1, 7] == float("inf") and got[2, 7] == float("-inf")    # 1.28e39 either way
+    scales[7] = 1e-3
+    want = binding.rago_q4_scores(codes, scales, q, 64)
+    rest = torch.arange(100, device="cuda") != 7
+    assert torch.equal(got[:, rest], want[:, rest])
+
+
 def test_a_bad_scale_or_query_stays_in_its_results():
     codes, scales = make_rows(300, 128, 32, torch.float32)
     q = make_queries(11, 128, torch.float32)
