@@ -387,8 +387,8 @@ rago_status rago_q4_rescore(const uint8_t* codes, const void* scales, rago_dtype
  * Backward pass of rago_q4_rescore (the rows are constants):
  *     grad_queries[q] = sum_j grad_dists[q][j] * row_j            (IP)
  *                       sum_j grad_dists[q][j] * 2 (query_q - row_j)   (L2)
- * over the candidates that are not missing; grad_dists of a missing one is not looked at.  L2 is taken as
- * 2 (query_q sum_j grad - sum_j grad row_j): its error is a few fp32 ulps of sum_j |grad| (|query| + |row|), not of the difference.
+ * over the candidates that are not missing; grad_dists of a missing one is not looked at.  The differences are taken number by number,
+ * so that the error stays relative to them where candidates lie near their query.
  *   grad_dists    dev fp32 [nq][k];  grad_queries  dev [nq][d], the type of the queries, summed in fp32 in a fixed order
  */
 rago_status rago_q4_rescore_backward(const uint8_t* codes, const void* scales, rago_dtype scale_dtype, int64_t N, int32_t d,

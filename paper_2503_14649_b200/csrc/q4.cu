@@ -560,8 +560,9 @@ __global__ void __launch_bounds__(Q4R_WARPS * 32) q4_rescore_kernel(const Q4Rows
 }
 
 // ---- gradient to the queries -----------------------------------------------------------------------------------------------
-// sum_j g_j row_j, from which the distance's is 2 (query sum_j g_j - that).  A thread owns 16 numbers, 8 bytes of a row; teams of
-// d / 16 threads take the candidates in turn, their sums meet in shared memory.  With few queries a cluster of CTAs shares the candidates
+// sum_j g_j row_j, or 2 sum_j g_j (query - row_j) for the distance, in that form: taken apart into 2 (query sum_j g_j - sum_j g_j row_j) it
+// would cancel where candidates are near, 3e-5 of the gradient for queries 0.01 |query| away.  A thread owns 16 numbers, 8 bytes of a row; teams of
+// d / 16 threads take the candidates in turn, their sums meet in shared memory, where the query lies too.  With few queries a cluster of CTAs shares the candidates
 // of one, and adds its sums up through distributed shared memory.  Missing candidates are left out when ids and gradients are staged, so
 // nothing of theirs is looked at.  Measured: 1024 queries' 100 candidates of 768 numbers 30 us, which is latency: ids, rows, sums of the
 // teams, one after the other, in a CTA that lives for 20 rows a team.
@@ -575,7 +576,6 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
     __shared__ uint32_t rows[Q4B_STAGE];
     __shared__ float gs[Q4B_STAGE];
     __shared__ int found[Q4B_THREADS / 32];
-    __shared__ float all_g[Q4B_THREADS / 32 + 1];
     grid_dependency_wait();
     grid_dependents_may_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, per_row = R.d / 16, team = tid / per_row, part = tid - team * per_row, row_bytes = R.d / 2;
@@ -584,10 +584,11 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
     const int j0 = (int)(((int64_t)k * rank) >> cluster_log2), j1 = (int)(((int64_t)k * (rank + 1)) >> cluster_log2);
     const bool works = team < teams;
     const Q4Float K = q4_float(k);
+    float* const xs = sums + teams * R.d;  // the query, for the distance
+    if (L2) q4_stage_query<QBF16>(xs, queries, q * R.d, R.d);
     F2 acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = f2(0.f, 0.f);
-    float g_sum = 0.f;  // this thread's share of sum g
     const int grp = part * 16 / R.group;
     for (int base = j0; base < j1; base += Q4B_STAGE) {
         const int n = min(Q4B_STAGE, j1 - base);
@@ -610,36 +611,42 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
                 at += __popc(mask & ((1u << lane) - 1u));
                 rows[at] = (uint32_t)id;
                 gs[at] = g;
-                g_sum += g;
             }
             __syncthreads();
         }
         if (works) {
-            constexpr int AT_ONCE = 4;  // rows whose numbers are asked for together
+            constexpr int AT_ONCE = L2 ? 2 : 4;  // rows whose numbers are asked for together (four of them with gradients and scales apart spill)
             for (int i = team; i < have; i += AT_ONCE * teams) {
                 uint2 w[AT_ONCE];
-                float f[AT_ONCE];
+                float f[AT_ONCE], g[AT_ONCE];  // scale, gradient; without L2 f is their product
 #pragma unroll
                 for (int a = 0; a < AT_ONCE; ++a) {
                     const int now = i + a * teams;
                     w[a] = make_uint2(0, 0);
-                    f[a] = 0.f;
+                    f[a] = g[a] = 0.f;
                     if (now < have) {
                         const size_t row = rows[now];
                         w[a] = *reinterpret_cast<const uint2*>(R.codes + row * row_bytes + part * 8);
-                        f[a] = gs[now] * load_f<SBF16>(R.scales, row * R.groups + grp);
+                        f[a] = load_f<SBF16>(R.scales, row * R.groups + grp);
+                        g[a] = gs[now];
                     }
                 }
 #pragma unroll
-                for (int a = 0; a < AT_ONCE; ++a) {
-                    const uint32_t word[2] = {w[a].x, w[a].y};
-                    const F2 f2x = f2(f[a], f[a]);
+                for (int p = 0; p < 4; ++p) {
+                    F2 x[2];
+                    if (L2) {
+                        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(xs + q4_spread(part / 2, part % 2 * 4 + p));
+                        x[0] = {v.x}; x[1] = {v.y};
+                    }
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
+                    for (int a = 0; a < AT_ONCE; ++a) {
+                        const uint32_t word = p / 2 ? w[a].y : w[a].x;
                         F2 v[2];
-                        q4_four(p & 1 ? word[p / 2] >> 16 : word[p / 2], K, v);
-                        acc[2 * p] = f2_fma(f2x, v[0], acc[2 * p]);
-                        acc[2 * p + 1] = f2_fma(f2x, v[1], acc[2 * p + 1]);
+                        q4_four(p & 1 ? word >> 16 : word, K, v);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (L2) acc[2 * p + h] = f2_fma(f2(g[a], g[a]), f2_fma(f2(-f[a], -f[a]), v[h], x[h]), acc[2 * p + h]);
+                            else acc[2 * p + h] = f2_fma(f2(g[a] * f[a], g[a] * f[a]), v[h], acc[2 * p + h]);
                     }
                 }
             }
@@ -649,16 +656,8 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<ulonglong2*>(sums + team * R.d + part * 16 + 4 * i) = make_ulonglong2(acc[2 * i].v, acc[2 * i + 1].v);
     }
-    if (L2) {
-        for (int o = 16; o; o >>= 1) g_sum += __shfl_xor_sync(0xffffffffu, g_sum, o);
-        if (lane == 0) all_g[warp] = g_sum;
-    }
     __syncthreads();
     // teams, then CTAs, in their order
-    if (L2 && tid == 0) {
-        for (int w = 1; w < (threads >> 5); ++w) g_sum += all_g[w];
-        all_g[Q4B_THREADS / 32] = g_sum;
-    }
     if (teams > 1)
         for (int i = tid; i < R.d; i += threads) {
             float v = sums[i];
@@ -673,12 +672,9 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
         for (int c = 0; c < cluster; ++c) v += __uint_as_float(lds_cluster_u32(mapa_shared(smem_u32(at), c)));
         return v;
     };
-    const float g_all = L2 ? over_cluster(&all_g[Q4B_THREADS / 32]) : 0.f;
     const int i0 = (R.d * rank) >> cluster_log2, i1 = (R.d * (rank + 1)) >> cluster_log2;
     for (int i = i0 + tid; i < i1; i += threads) {
-        float v = over_cluster(sums + i);
-        // without candidates 0, whatever the query
-        if (L2) v = 2.f * (g_all == 0.f ? -v : fmaf(load_f<QBF16>(queries, q * R.d + i), g_all, -v));
+        const float v = over_cluster(sums + i) * (L2 ? 2.f : 1.f);
         if (QBF16) static_cast<__nv_bfloat16*>(out)[q * R.d + i] = __float2bfloat16_rn(v);
         else static_cast<float*>(out)[q * R.d + i] = v;
     }
@@ -908,10 +904,15 @@ extern "C" rago_status rago_q4_rescore_backward(const uint8_t* codes, const void
     int cluster_log2 = 0;
     while ((1 << cluster_log2) < Q4B_MAX_CLUSTER && (int64_t)nq << cluster_log2 < 2 * sms && k >= (int64_t)(8 * teams) << cluster_log2) ++cluster_log2;
     const int cluster = 1 << cluster_log2;
+    const size_t smem = (size_t)(teams + (metric == RAGO_L2 ? 1 : 0)) * d * 4;  // the teams' sums, the query: at most 64 KB
     e = q4_types(query_dtype, scale_dtype, metric, [&](auto qb, auto sb, auto l2) {
         auto kernel = q4_rescore_backward_kernel<decltype(qb)::value, decltype(sb)::value, decltype(l2)::value>;
+        if (smem > 40 * 1024) {  // long rows; 48 KB go without asking, some of them to the kernel's own arrays
+            const cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (r != cudaSuccess) return r;
+        }
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)((int64_t)nq * cluster)); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = (size_t)teams * d * 4; cfg.stream = s;
+        cfg.gridDim = dim3((unsigned)((int64_t)nq * cluster)); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;

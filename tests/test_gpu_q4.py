@@ -4,8 +4,8 @@ the definition in 64 bits.
 Tolerances.  u = 2^-24.  A sum of n fp32 terms in any order is off by at most (n - 1) u sum|terms| (first order); a product adds
 u, the scale another u.  So |error| <= (n + 4) u * sum of the magnitudes, with 5 % for the second order.  An L2 term is
 t = x - s (c - 8) in one rounding, squared: 3 u more at most.  A result stored in bf16 is off by half a step more, 2^-8.
-The gradient of k distances is 2 (x sum g - sum g w): k terms of either kind, each off by (k + 3) u of the sum of its magnitudes,
-and two roundings behind them: (k + 6) u * 2 sum |g| (|x| + |w|)."""
+The gradient of k distances is 2 sum g (x - w), the difference in one rounding: (k + 6) u * 2 sum |g| |x - w|, which check_candidates,
+written for 2 (x sum g - sum g w), bounds by (k + 6) u * 2 sum |g| (|x| + |w|)."""
 
 import pytest
 import torch
@@ -259,6 +259,30 @@ def test_a_query_that_is_a_stored_row_has_distance_zero():
     got = binding.rago_q4_rescore(codes, scales, q, ids, 64, "l2")
     # x is the rounded product, the row the exact one: each term is at most (u |x|)^2
     assert (got[:, 0].double() <= SECOND_ORDER * (U ** 2) * q.double().square().sum(1)).all()
+
+
+@pytest.mark.parametrize("query", ["f32", "bf16"])
+@pytest.mark.parametrize("near", [1.0, 0.01, 1e-3])
+@pytest.mark.parametrize("nq,k,d", [(1, 700, 96), (5, 33, 160), (300, 100, 768), (2, 9, 8192)])
+def test_the_gradient_of_near_candidates(nq, k, d, near, query):
+    """Candidates that lie `near` times its length from their query.  A term is g (x - s (c - 8)), the difference in one rounding, so the
+    error is relative to the differences, not to query and row: (k + 6) u * 2 sum |g| |x - w|."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes, scales = make_rows(400, d, 32, torch.float32)
+    codes[:] = codes[0].clone()
+    scales[:] = scales[0].clone() * (1 + near * torch.rand(scales.shape, generator=g, device="cuda"))
+    w = values64(codes, scales, 32)
+    q = (w[0] * (1 + near * torch.randn((nq, d), generator=g, device="cuda").double())).to(DTYPES[query])
+    ids = make_ids(nq, k, 400)
+    grad = torch.randn((nq, k), generator=g, device="cuda")
+    there = (ids >= 0) & (ids < 400)
+    got = binding.rago_q4_rescore_backward(codes, scales, q, ids, 32, "l2", grad).double()
+    for r in range(nq):
+        terms = 2 * grad[r][there[r]].double()[:, None] * (q[r].double() - w[ids[r][there[r]]])
+        tol = SECOND_ORDER * (k + 6) * U * terms.abs().sum(0)
+        if query == "bf16":
+            tol = tol + 2.0 ** -8 * terms.sum(0).abs() + 1e-38
+        assert ((got[r] - terms.sum(0)).abs() <= tol).all(), r
 
 
 def test_results_do_not_change_from_call_to_call():
