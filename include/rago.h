@@ -418,10 +418,11 @@ rago_status rago_q4_rescore_backward(const uint8_t* codes, const void* scales, r
  * NaN or infinite.  (exp(x) below 2^-126 of the row's largest is 0, and so is pi then, wherever the candidate stands.)  A NaN or
  * +infinity among the candidates makes that query's results NaN, and no other's.
  *   workspace   dev, 256-byte aligned, rago_policy_workspace_bytes(...) bytes: the partial sums of long rows (0 bytes, and then
- *               NULL will do, for rows of up to 16 384 candidates).  Two calls that overlap on the GPU need distinct ones
+ *               NULL will do, for rows of up to RAGO_POLICY_SPAN candidates).  Two calls that overlap on the GPU need distinct ones
  * C >= 1, nq * C < 2^40, 0 <= G <= 1024.  Sums are fp32, in a fixed order.
  */
 #define RAGO_POLICY_STATS 4
+#define RAGO_POLICY_SPAN 16384
 rago_status rago_policy_loss(const void* scores, const void* ref_scores, rago_dtype dtype, const int64_t* ids, int32_t nq,
                              int32_t C, float scale, const int32_t* chosen, const float* old_logp, const float* advantage,
                              int32_t G, float clip_low, float clip_high, float* out_policy, float* out_kl, float* out_logp,

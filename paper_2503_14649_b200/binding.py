@@ -317,6 +317,7 @@ def rago_merge_results(part_ids: torch.Tensor, part_dists: torch.Tensor, k_out: 
 # ---- what is done with the answers of a search -------------------------------------------------------------------------
 
 POLICY_STATS = BALANCE_STATS = 4
+POLICY_SPAN = 16_384  # longest row that needs no workspace
 _FLOATS = {torch.float32: RAGO_F32, torch.bfloat16: RAGO_BF16}
 
 
@@ -434,13 +435,15 @@ def rago_policy_loss(scores: torch.Tensor, chosen: torch.Tensor, old_logp: torch
     policy, kl = old_logp.new_empty(nq), old_logp.new_empty(nq)
     logp = torch.empty_like(old_logp)
     stats = old_logp.new_empty(nq, POLICY_STATS)
-    if workspace is None and C > 16_384:
+    if workspace is not None:
+        _expect("workspace", workspace, workspace.shape, (workspace.dtype,), dev)
+    elif C > POLICY_SPAN:
         workspace = scores.new_empty(rago_policy_workspace_bytes(nq, C), dtype=torch.uint8)
     _check(lib().rago_policy_loss(scores.data_ptr(), None if ref_scores is None else ref_scores.data_ptr(), _FLOATS[scores.dtype],
                                   None if ids is None else ids.data_ptr(), nq, C, scale, chosen.data_ptr(), old_logp.data_ptr(),
                                   advantage.data_ptr(), G, clip_low, clip_high, policy.data_ptr(), kl.data_ptr(), logp.data_ptr(),
                                   stats.data_ptr(), None if workspace is None else workspace.data_ptr(),
-                                  0 if workspace is None else workspace.numel(), _stream()))
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
     return PolicyLoss(policy, kl, logp, stats)
 
 

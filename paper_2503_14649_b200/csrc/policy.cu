@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(POLICY_WARPS * 32) policy_forward_short_kernel
 // Long rows: CTAs of POLICY_SPAN candidates.  A row of one span is finished by its CTA; the sums of several go to the workspace, and the
 // kernel behind joins them, in their order.  (Clusters whose first CTA joined them through distributed shared memory needed no
 // workspace, but 37 rows in clusters of 8 did not fit the GPU's parts at once: 79 us instead of 47 for 1 000 003 scores.)
-constexpr int POLICY_SPAN = 16384, POLICY_THREADS = 256;
+constexpr int POLICY_SPAN = RAGO_POLICY_SPAN, POLICY_THREADS = 256;
 
 template <bool BF16, bool REF>
 __device__ __forceinline__ void policy_finish(const PolicyArgs& A, int q, PolicySums S, float* terms, float* __restrict__ out_policy, float* __restrict__ out_kl,

@@ -156,6 +156,44 @@ def test_tensors_on_the_host_and_of_other_shapes_or_types():
         binding.rago_list_balance(x, ch[0], 1.0)
 
 
+def test_a_workspace_that_the_library_would_not_write_as_it_is(monkeypatch):
+    """The other tensors stand for ones on the GPU here: the workspace is what is refused."""
+    x, ch, f = torch.zeros((2, 20_000)), torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2, 3))
+    expect = binding._expect
+
+    def only_the_workspace(name, t, *a):
+        if name == "workspace":
+            expect(name, t, *a)
+
+    monkeypatch.setattr(binding, "_expect", only_the_workspace)
+    monkeypatch.setattr(binding, "lib", lambda: pytest.fail("the library was called"))
+    for w in (torch.zeros(4096, dtype=torch.uint8), torch.zeros(1024), torch.zeros(8192, dtype=torch.uint8)[::2], torch.zeros((2, 2048), dtype=torch.uint8)):
+        with pytest.raises(ValueError, match="workspace"):
+            binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2, workspace=w)
+
+
+def test_the_binding_knows_which_rows_need_a_workspace():
+    assert binding.rago_policy_workspace_bytes(7, binding.POLICY_SPAN) == 0 < binding.rago_policy_workspace_bytes(7, binding.POLICY_SPAN + 1)
+
+
+@pytest.mark.gpu
+def test_workspaces_on_the_gpu():
+    x, ch, f = torch.randn((2, 20_000), device="cuda"), torch.zeros((2, 3), dtype=torch.int32, device="cuda"), torch.zeros((2, 3), device="cuda")
+    need = binding.rago_policy_workspace_bytes(2, 20_000)
+    want = binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2)
+    room = torch.full((need + 64,), 7, dtype=torch.uint8, device="cuda")
+    got = binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2, workspace=room[:need])
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and (room[need:] == 7).all()
+    numbers = torch.zeros((2, need // 8), device="cuda")  # any contiguous tensor will do
+    got = binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2, workspace=numbers)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    for w in (torch.zeros(need, dtype=torch.uint8), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2, workspace=w)
+    with pytest.raises(binding.RagoError):
+        binding.rago_policy_loss(x, ch, f, f, 1.0, 0.2, 0.2, workspace=room[:need - 1])
+
+
 @pytest.mark.gpu
 def test_tensors_on_the_gpu_of_other_shapes_types_or_orders():
     codes, scales = torch.zeros((8, 32), dtype=torch.uint8, device="cuda"), torch.zeros((8, 2), device="cuda")
