@@ -356,6 +356,7 @@ rago_status rago_merge_results(const int64_t* part_ids, const float* part_dists,
  *   d a multiple of 32, d <= 8192; group 32, 64 or 128; N < 2^31
  * Products and sums are fp32 whatever the types.  A NaN or infinite scale or
  * query makes the results that use it NaN or infinite, and no others.  These calls need no workspace.
+ * Here and in the calls below, a pointer without an alignment of its own is aligned to its type (RAGO_EALIGN otherwise).
  */
 
 /*
@@ -389,7 +390,7 @@ rago_status rago_q4_rescore(const uint8_t* codes, const void* scales, rago_dtype
  *                       sum_j grad_dists[q][j] * 2 (query_q - row_j)   (L2)
  * over the candidates that are not missing; grad_dists of a missing one is not looked at.  The differences are taken number by number,
  * so that the error stays relative to them where candidates lie near their query.
- *   grad_dists    dev fp32 [nq][k];  grad_queries  dev [nq][d], the type of the queries, summed in fp32 in a fixed order
+ *   grad_dists    dev fp32 [nq][k];  grad_queries  dev [nq][d], 16-byte aligned, the type of the queries, summed in fp32 in a fixed order
  */
 rago_status rago_q4_rescore_backward(const uint8_t* codes, const void* scales, rago_dtype scale_dtype, int64_t N, int32_t d,
                                      int32_t group, const void* queries, rago_dtype query_dtype, int32_t nq,

@@ -679,6 +679,8 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
     if ((long long)nq * nprobe >= (1LL << 31)) return balance_fail(RAGO_EUNSUPPORTED, "nq * nprobe = %lld exceeds 2^31 - 1", (long long)nq * nprobe);
     if ((nq > 0 && !lists) || !out_loss || !out_counts || !out_stats) return balance_fail(RAGO_EINVAL, "null pointer");
     if (reinterpret_cast<uintptr_t>(out_stats) % 16) return balance_fail(RAGO_EALIGN, "out_stats need 16-byte alignment");
+    if ((reinterpret_cast<uintptr_t>(lists) | reinterpret_cast<uintptr_t>(out_loss) | reinterpret_cast<uintptr_t>(out_counts)) % 4)
+        return balance_fail(RAGO_EALIGN, "lists, out_loss or out_counts are not aligned to their type");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     float4* stats = reinterpret_cast<float4*>(out_stats);
     BalanceTotals* totals = reinterpret_cast<BalanceTotals*>(stats + nq);
@@ -734,6 +736,7 @@ extern "C" rago_status rago_list_balance_backward(const void* logits, rago_dtype
     if (st != RAGO_OK || nq == 0) return st;
     if (!counts || !stats || !grad_loss || !grad_logits) return balance_fail(RAGO_EINVAL, "null pointer");
     if (reinterpret_cast<uintptr_t>(stats) % 16) return balance_fail(RAGO_EALIGN, "stats need 16-byte alignment");
+    if ((reinterpret_cast<uintptr_t>(counts) | reinterpret_cast<uintptr_t>(grad_loss)) % 4) return balance_fail(RAGO_EALIGN, "counts or grad_loss are not aligned to their type");
     if (reinterpret_cast<uintptr_t>(grad_logits) % (dtype == RAGO_F32 ? 4 : 2)) return balance_fail(RAGO_EALIGN, "grad_logits are not aligned to their type");
     const float4* st4 = reinterpret_cast<const float4*>(stats);
     const BalanceTotals* totals = reinterpret_cast<const BalanceTotals*>(st4 + nq);

@@ -516,6 +516,8 @@ static rago_status policy_fail(rago_status st, const char* what, long long v = 0
     return st;
 }
 
+static bool policy_off(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; }
+
 static rago_status policy_check(const void* scores, const void* ref, rago_dtype dtype, const int64_t* ids, int32_t nq, int32_t C, float scale,
                                 const int32_t* chosen, const float* old_logp, const float* advantage, int32_t G, float clip_low,
                                 float clip_high, PolicyArgs* A) {
@@ -533,6 +535,7 @@ static rago_status policy_check(const void* scores, const void* ref, rago_dtype 
     const uintptr_t unit = dtype == RAGO_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(scores) % unit || reinterpret_cast<uintptr_t>(ref) % unit || reinterpret_cast<uintptr_t>(ids) % 8)
         return policy_fail(RAGO_EALIGN, "scores, ref_scores or ids are not aligned to their type");
+    if (policy_off(chosen) || policy_off(old_logp) || policy_off(advantage)) return policy_fail(RAGO_EALIGN, "chosen, old_logp or advantage are not aligned to their type");
     A->scores = scores; A->ref = ref; A->ids = ids; A->lowest = scale > 0.f ? -INFINITY : INFINITY; A->unit = scale > 0.f ? 0x1p-24f : -0x1p-24f;
     A->nq = nq; A->C = C; A->G = G;
     A->a = (float)((double)scale * 1.44269504088896340736); A->scale = scale;
@@ -584,6 +587,7 @@ extern "C" rago_status rago_policy_loss(const void* scores, const void* ref_scor
     if (st != RAGO_OK || nq == 0) return st;
     if (!out_policy || !out_kl || !out_stats || (G > 0 && !out_logp)) return policy_fail(RAGO_EINVAL, "null pointer");
     if (reinterpret_cast<uintptr_t>(out_stats) % 16) return policy_fail(RAGO_EALIGN, "out_stats need 16-byte alignment");
+    if (policy_off(out_policy) || policy_off(out_kl) || policy_off(out_logp)) return policy_fail(RAGO_EALIGN, "out_policy, out_kl or out_logp are not aligned to their type");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     float4* stats = reinterpret_cast<float4*>(out_stats);
     size_t need = 0;
@@ -617,6 +621,8 @@ extern "C" rago_status rago_policy_loss_backward(const void* scores, const void*
     if (st != RAGO_OK || nq == 0) return st;
     if (!stats || !grad_scores || (G > 0 && (!logp || !grad_policy)) || (ref_scores && (!kl || !grad_kl))) return policy_fail(RAGO_EINVAL, "null pointer");
     if (reinterpret_cast<uintptr_t>(stats) % 16) return policy_fail(RAGO_EALIGN, "stats need 16-byte alignment");
+    if (policy_off(kl) || policy_off(logp) || policy_off(grad_policy) || policy_off(grad_kl))
+        return policy_fail(RAGO_EALIGN, "kl, logp, grad_policy or grad_kl are not aligned to their type");
     if (reinterpret_cast<uintptr_t>(grad_scores) % (dtype == RAGO_F32 ? 4 : 2)) return policy_fail(RAGO_EALIGN, "grad_scores are not aligned to their type");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const PolicyGrads D = {kl, logp, reinterpret_cast<const float4*>(stats), grad_policy, grad_kl, grad_scores};

@@ -712,6 +712,7 @@ static rago_status q4_check_lists(int32_t nq, const int64_t* ids, int32_t k, int
     if (metric != RAGO_L2 && metric != RAGO_IP) return fail_q4(RAGO_EINVAL, "metric = %lld is neither L2 nor IP", metric);
     if ((long long)nq * k >= (1LL << 31)) return fail_q4(RAGO_EUNSUPPORTED, "nq * k = %lld exceeds 2^31 - 1", (long long)nq * k);
     if (nq > 0 && (!ids || !dists)) return fail_q4(RAGO_EINVAL, "null pointer", 0);
+    if (reinterpret_cast<uintptr_t>(ids) % 8 || reinterpret_cast<uintptr_t>(dists) % 4) return fail_q4(RAGO_EALIGN, "ids or distances are not aligned to their type", 0);
     return RAGO_OK;
 }
 
@@ -845,6 +846,7 @@ extern "C" rago_status rago_q4_scores(const uint8_t* codes, const void* scales, 
     if (st != RAGO_OK) return st;
     if (N == 0 || nq == 0) return RAGO_OK;
     if (!out_scores) return fail_q4(RAGO_EINVAL, "null pointer", 0);
+    if (reinterpret_cast<uintptr_t>(out_scores) % 4) return fail_q4(RAGO_EALIGN, "out_scores are not aligned to their type", 0);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     int dev = 0, sms = 0, launches = 0;
     cudaError_t e = cudaGetDevice(&dev);

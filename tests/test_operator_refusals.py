@@ -132,6 +132,20 @@ def test_list_balance_inputs_and_outputs():
     assert call("rago_list_balance_backward", BALANCE_BACKWARD, grad=A + 2) == EALIGN
 
 
+@pytest.mark.parametrize("name,defaults,pointers", [
+    ("rago_q4_scores", SCORES, {"out": 4}),
+    ("rago_q4_rescore", RESCORE, {"ids": 8, "out": 4}),
+    ("rago_q4_rescore_backward", RESCORE_BACKWARD, {"ids": 8, "grad": 4}),
+    ("rago_policy_loss", POLICY, {"chosen": 4, "old": 4, "adv": 4, "policy": 4, "kl": 4, "logp": 4}),
+    ("rago_policy_loss_backward", POLICY_BACKWARD, {"chosen": 4, "old": 4, "adv": 4, "kl": 4, "logp": 4, "grad_policy": 4, "grad_kl": 4}),
+    ("rago_list_balance", BALANCE, {"lists": 4, "loss": 4, "counts": 4}),
+    ("rago_list_balance_backward", BALANCE_BACKWARD, {"counts": 4, "grad_loss": 4})])
+def test_pointers_that_are_not_aligned_to_their_type(name, defaults, pointers):
+    for pointer, size in pointers.items():
+        for off in (1, 2, size // 2, size - 1):
+            assert call(name, defaults, **{pointer: A + off}) == EALIGN, pointer
+
+
 # ---- the binding: tensors that the library would read as something else ----------------------------------------------------
 
 def test_tensors_on_the_host_and_of_other_shapes_or_types():
