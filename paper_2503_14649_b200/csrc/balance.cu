@@ -227,7 +227,7 @@ __device__ __forceinline__ void balance_window(const int32_t* __restrict__ count
     const bool aligned = (reinterpret_cast<uintptr_t>(counts) & 15) == 0;
     if (aligned && shift == 0) {
         LogitPiece<BF16>::counts(counts, start, base, v);
-    } else if (aligned && start - shift + UNIT + 4 <= nlist) {
+    } else if (aligned && start - shift <= nlist - (UNIT + 4)) {
         int w[UNIT + 4];
 #pragma unroll
         for (int i = 0; i < UNIT + 4; i += 4) *reinterpret_cast<int4*>(w + i) = *reinterpret_cast<const int4*>(counts + start - shift + i);
@@ -271,8 +271,8 @@ __device__ __forceinline__ void balance_sweep(BalanceSums& S, const void* __rest
         P::values(w, v);
         balance_add<P::UNIT>(S, v, c, a);
     }
-    for (int i = first; i < head + nlist - tail; i += stride) {
-        const int l = i < head ? i : tail + i - head;
+    for (int i = first; i < head + (nlist - tail); i += stride) {
+        const int l = i < head ? i : tail + (i - head);
         const float v[1] = {load_l<BF16>(logits, row + l)}, c[1] = {(float)(counts[l] - base)};
         balance_add<1>(S, v, c, a);
     }
@@ -404,8 +404,8 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
             pieces[r] = (nlist - head[r]) / P::UNIT;
             most = max(most, pieces[r]);
             const int tail = head[r] + pieces[r] * P::UNIT;
-            for (int i = tid; i < head[r] + nlist - tail; i += THREADS) {
-                const int l = i < head[r] ? i : tail + i - head[r];
+            for (int i = tid; i < head[r] + (nlist - tail); i += THREADS) {
+                const int l = i < head[r] ? i : tail + (i - head[r]);
                 const float v[1] = {load_l<BF16>(logits, row + l)}, c[1] = {(float)(counts[l] - base)};
                 balance_add<1>(S[r], v, c, a);
             }
@@ -554,8 +554,8 @@ __global__ void __launch_bounds__(BALANCE_THREADS) balance_backward_long_kernel(
             P::store(out, row + l, v);
         }
         if (span == 0)
-            for (int i = threadIdx.x; i < head + nlist - tail; i += BALANCE_THREADS) {
-                const int l = i < head ? i : tail + i - head;
+            for (int i = threadIdx.x; i < head + (nlist - tail); i += BALANCE_THREADS) {
+                const int l = i < head ? i : tail + (i - head);
                 float v[1] = {0.f}, c[1] = {(float)(counts[l] - B.base)};
                 if (counted) {
                     v[0] = load_l<BF16>(logits, row + l);
@@ -686,21 +686,21 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
     BalanceTotals* totals = reinterpret_cast<BalanceTotals*>(stats + nq);
     uint32_t* ticket = reinterpret_cast<uint32_t*>(totals);  // the first word
     const int64_t slots = (int64_t)nq * nprobe;
-    int ranges = (int)(((int64_t)nlist + BALANCE_RANGE_LISTS - 1) / BALANCE_RANGE_LISTS), launches = 0;
+    int ranges = (int)parts_of(nlist, BALANCE_RANGE_LISTS), launches = 0;
     ranges = ranges < BALANCE_RANGE_CTAS ? ranges : BALANCE_RANGE_CTAS;
-    const int range = (int)(((int64_t)nlist + ranges - 1) / ranges);
+    const int range = (int)parts_of(nlist, ranges);
     cudaError_t e;
     if (slots <= BALANCE_RANGE_SLOTS && range <= BALANCE_SHARED_LISTS) {
-        e = launch_overlapped(balance_count_ranges_kernel, dim3((unsigned)((nlist + range - 1) / range)), dim3(BALANCE_RANGE_THREADS), (size_t)range * 4, s, lists, valid,
+        e = launch_overlapped(balance_count_ranges_kernel, dim3((unsigned)parts_of(nlist, range)), dim3(BALANCE_RANGE_THREADS), (size_t)range * 4, s, lists, valid,
                               nq, nprobe, nlist, range, out_counts, totals, ticket);
         ++launches;
     } else {
         const bool shared = nlist <= BALANCE_SHARED_LISTS;
-        e = launch_overlapped(balance_clear_kernel, dim3((unsigned)(((int64_t)nlist + BALANCE_THREADS - 1) / BALANCE_THREADS)), dim3(BALANCE_THREADS), 0, s,
+        e = launch_overlapped(balance_clear_kernel, dim3((unsigned)parts_of(nlist, BALANCE_THREADS)), dim3(BALANCE_THREADS), 0, s,
                               out_counts, nlist, totals, ticket);
         ++launches;
         if (e == cudaSuccess && slots) {
-            const int64_t ctas = (slots + 8 * BALANCE_COUNT_THREADS - 1) / (8 * BALANCE_COUNT_THREADS);
+            const int64_t ctas = parts_of(slots, 8 * BALANCE_COUNT_THREADS);
             e = launch_overlapped(shared ? balance_count_kernel<true> : balance_count_kernel<false>, dim3((unsigned)(ctas < 4096 ? ctas : 4096)), dim3(BALANCE_COUNT_THREADS),
                                   shared ? (size_t)nlist * 4 : 0, s, lists, valid, nq, nprobe, nlist, out_counts, totals);
             ++launches;
@@ -712,7 +712,7 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
         auto rows = [&](auto bf16) {
             constexpr bool B = decltype(bf16)::value;
             auto launch = [&](auto kernel, int per_cta, int threads) {
-                return launch_overlapped(kernel, dim3((unsigned)((nq + per_cta - 1) / per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts,
+                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts,
                                          totals, ticket, stats, out_loss);
             };
             if (nlist <= (B ? 128 : 64)) return launch(balance_short_rows_kernel<B, 8, 1>, 32, BALANCE_THREADS);
@@ -747,23 +747,23 @@ extern "C" rago_status rago_list_balance_backward(const void* logits, rago_dtype
         const int64_t pieces = nlist / (B ? 8 : 4), per = BALANCE_THREADS;
         if (!whole) {
             if (pieces >= per) {  // 4096 x 65 533 in bf16: 260 us, by slots 334 (267 now); 16 384 x 61: 17.6, by slots 5.2
-                const int spans = (int)((pieces + per - 1) / per);
-                return launch_overlapped(balance_backward_long_kernel<B>, dim3((unsigned)((int64_t)spans * ((nq + BALANCE_ANY_ROWS - 1) / BALANCE_ANY_ROWS))),
+                const int spans = (int)parts_of(pieces, per);
+                return launch_overlapped(balance_backward_long_kernel<B>, dim3((unsigned)(spans * parts_of(nq, BALANCE_ANY_ROWS))),
                                          dim3(BALANCE_THREADS), 0, s, logits, nq, nlist, spans, a, scale, valid, counts, st4, totals, grad_loss, grad_logits);
             }
             const int64_t slots = pieces + 2;
             int tile_log2 = 1;
             while (tile_log2 < 8 && (1 << tile_log2) < slots) ++tile_log2;
             const int tiles = (int)((slots + (1 << tile_log2) - 1) >> tile_log2), rows = 2 * (BALANCE_THREADS >> tile_log2);
-            return launch_overlapped(balance_backward_short_kernel<B>, dim3((unsigned)((int64_t)tiles * ((nq + rows - 1) / rows))), dim3(BALANCE_THREADS), 0, s, logits,
+            return launch_overlapped(balance_backward_short_kernel<B>, dim3((unsigned)(tiles * parts_of(nq, rows))), dim3(BALANCE_THREADS), 0, s, logits,
                                      nq, nlist, tiles, tile_log2, a, scale, valid, counts, st4, totals, grad_loss, grad_logits);
         }
         auto launch = [&](auto kernel, int64_t ctas) {
             return launch_overlapped(kernel, dim3((unsigned)ctas), dim3(BALANCE_THREADS), 0, s, logits, nq, nlist, a, scale, valid, counts, st4, totals, grad_loss,
                                      grad_logits);
         };
-        if ((int64_t)nq * pieces >= (1 << 20)) return launch(balance_backward_kernel<B, 4>, ((nq + 3) / 4 * pieces + per - 1) / per);
-        return launch(balance_backward_kernel<B, 1>, (nq * pieces + per - 1) / per);
+        if ((int64_t)nq * pieces >= (1 << 20)) return launch(balance_backward_kernel<B, 4>, parts_of(parts_of(nq, 4) * pieces, per));
+        return launch(balance_backward_kernel<B, 1>, parts_of(nq * pieces, per));
     };
     return balance_done(dtype == RAGO_BF16 ? go(std::true_type{}) : go(std::false_type{}), 1, "list balance backward kernel");
 }

@@ -114,6 +114,8 @@ __host__ __device__ inline unsigned long long make_key(float score_smaller_is_be
 }
 
 __host__ __device__ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+// Parts of `per` that n makes up; in 64 bits, since n + per - 1 may not fit 32 where n does
+__host__ __device__ inline int64_t parts_of(int64_t n, int64_t per) { return (n + per - 1) / per; }
 
 #ifdef __CUDACC__
 // ---- shared-memory address / mbarrier / bulk-copy wrappers ----------------------------------

@@ -416,12 +416,11 @@ __device__ __forceinline__ void policy_put_one(const PolicyArgs& A, const Policy
     else static_cast<float*>(D.out)[at] = g;
 }
 
-// Candidates begin .. end - 1 of a row, shared by `stride` threads.  Pieces follow the boundaries of the output.
+// Candidates begin .. begin + n - 1 of a row, shared by `stride` threads.  Pieces follow the boundaries of the output.
 template <bool BF16, bool REF, bool IDS>
-__device__ __forceinline__ void policy_back_sweep(const PolicyArgs& A, const PolicyGrads& D, const PolicyBack& B, int q, int begin, int end, int first, int stride) {
+__device__ __forceinline__ void policy_back_sweep(const PolicyArgs& A, const PolicyGrads& D, const PolicyBack& B, int q, int begin, int n, int first, int stride) {
     using P = Piece<BF16>;
     const size_t row = (size_t)q * A.C + begin;
-    const int n = end - begin;
     int head = P::head(D.out, row);
     if (head > n) head = n;
     const int pieces = (n - head) / P::UNIT, tail = head + pieces * P::UNIT;
@@ -476,11 +475,11 @@ __global__ void __launch_bounds__(POLICY_BACK_THREADS) policy_backward_long_kern
     __shared__ float warp_part[POLICY_BACK_THREADS / 32];
     grid_dependency_wait();
     grid_dependents_may_launch();
-    const int q = blockIdx.x / spans, begin = blockIdx.x % spans * POLICY_BACK_SPAN, end = min(A.C, begin + POLICY_BACK_SPAN), tid = threadIdx.x;
+    const int q = blockIdx.x / spans, begin = blockIdx.x % spans * POLICY_BACK_SPAN, here = min(A.C - begin, POLICY_BACK_SPAN), tid = threadIdx.x;
     // the span's lines are asked for before the samples are looked at
     constexpr int SIZE = BF16 ? 2 : 4, LINE = 128 / SIZE;
-    for (int i = begin + tid * LINE; i < end; i += POLICY_BACK_THREADS * LINE) {
-        const size_t at = (size_t)q * A.C + i;
+    for (int i = tid * LINE; i < here; i += POLICY_BACK_THREADS * LINE) {
+        const size_t at = (size_t)q * A.C + begin + i;
         asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(A.scores) + at * SIZE));
         if (REF) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(A.ref) + at * SIZE));
     }
@@ -497,11 +496,11 @@ __global__ void __launch_bounds__(POLICY_BACK_THREADS) policy_backward_long_kern
     H = 0.f;
     for (int w = 0; w < POLICY_BACK_THREADS / 32; ++w) H += warp_part[w];
     const PolicyBack B = policy_back<REF>(A, D, q, H);
-    policy_back_sweep<BF16, REF, IDS>(A, D, B, q, begin, end, tid, POLICY_BACK_THREADS);
+    policy_back_sweep<BF16, REF, IDS>(A, D, B, q, begin, here, tid, POLICY_BACK_THREADS);
     __syncthreads();
     for (int t = tid; t < A.G; t += POLICY_BACK_THREADS) {  // the first sample of a candidate writes the sum of all of its samples
         const int c = at_of[t];
-        if (c < begin || c >= end) continue;
+        if (c < begin || c - begin >= here) continue;
         bool is_first = true;
         for (int u = 0; u < t && is_first; ++u) is_first = at_of[u] != c;
         if (!is_first) continue;
@@ -527,7 +526,7 @@ static rago_status policy_check(const void* scores, const void* ref, rago_dtype 
     if (dtype != RAGO_F32 && dtype != RAGO_BF16) return policy_fail(RAGO_EINVAL, "dtype = %lld is neither F32 nor BF16", dtype);
     if (!(scale - scale == 0.f) || scale == 0.f) return policy_fail(RAGO_EINVAL, "scale must be finite and not 0");
     if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f)) return policy_fail(RAGO_EINVAL, "clip_low must lie in [0, 1] and clip_high be at least 0");
-    if ((long long)nq * ((C + 8191LL) / 8192) >= (1LL << 31)) return policy_fail(RAGO_EUNSUPPORTED, "nq * C is too large for one launch");
+    if (nq * parts_of(C, POLICY_BACK_SPAN) >= (1LL << 31)) return policy_fail(RAGO_EUNSUPPORTED, "nq * C is too large for one launch");
     if (G > POLICY_MAX_G) return policy_fail(RAGO_EUNSUPPORTED, "G = %lld exceeds 1024", G);
     if ((long long)nq * C >= (1LL << 40)) return policy_fail(RAGO_EUNSUPPORTED, "nq * C = %lld is 2^40 or more", (long long)nq * C);
     if (nq > 0 && !scores) return policy_fail(RAGO_EINVAL, "scores are null");
@@ -573,7 +572,7 @@ extern "C" rago_status rago_policy_workspace_bytes(int32_t nq, int32_t C, size_t
     if (!out_bytes) return policy_fail(RAGO_EINVAL, "out_bytes is null");
     if (nq < 0) return policy_fail(RAGO_EINVAL, "nq = %lld is negative", nq);
     if (C < 1) return policy_fail(RAGO_EINVAL, "C = %lld must be at least 1", C);
-    const size_t spans = ((size_t)C + POLICY_SPAN - 1) / POLICY_SPAN;
+    const size_t spans = (size_t)parts_of(C, POLICY_SPAN);
     *out_bytes = spans > 1 ? align_up((size_t)nq * spans * sizeof(PolicySums), 256) : 0;
     return RAGO_OK;
 }
@@ -597,11 +596,11 @@ extern "C" rago_status rago_policy_loss(const void* scores, const void* ref_scor
         if (reinterpret_cast<uintptr_t>(workspace) % 256) return policy_fail(RAGO_EALIGN, "workspace needs 256-byte alignment");
         if (workspace_bytes < need) return policy_fail(RAGO_ENOMEM, "workspace is smaller than the %lld bytes needed", (long long)need);
     }
-    const int spans = (C + POLICY_SPAN - 1) / POLICY_SPAN;
+    const int spans = (int)parts_of(C, POLICY_SPAN);
     return policy_done(policy_variant(A, dtype, [&](auto b, auto r, auto i) {
         constexpr bool B = decltype(b)::value, R = decltype(r)::value, I = decltype(i)::value;
         if (C <= POLICY_SHORT)
-            return launch_overlapped(policy_forward_short_kernel<B, R, I>, dim3((unsigned)((nq + POLICY_WARPS - 1) / POLICY_WARPS)), dim3(POLICY_WARPS * 32), 0, s, A,
+            return launch_overlapped(policy_forward_short_kernel<B, R, I>, dim3((unsigned)parts_of(nq, POLICY_WARPS)), dim3(POLICY_WARPS * 32), 0, s, A,
                                      out_policy, out_kl, out_logp, stats);
         PolicySums* sums = static_cast<PolicySums*>(workspace);
         const cudaError_t e = launch_overlapped(policy_forward_long_kernel<B, R, I>, dim3((unsigned)((int64_t)nq * spans)), dim3(POLICY_THREADS), 0, s, A, spans, sums,
@@ -629,9 +628,9 @@ extern "C" rago_status rago_policy_loss_backward(const void* scores, const void*
     return policy_done(policy_variant(A, dtype, [&](auto b, auto r, auto i) {
         constexpr bool B = decltype(b)::value, R = decltype(r)::value, I = decltype(i)::value;
         if (C <= POLICY_SHORT && G <= 32)
-            return launch_overlapped(policy_backward_short_kernel<B, R, I>, dim3((unsigned)((nq + POLICY_WARPS - 1) / POLICY_WARPS)), dim3(POLICY_WARPS * 32), 0, s,
+            return launch_overlapped(policy_backward_short_kernel<B, R, I>, dim3((unsigned)parts_of(nq, POLICY_WARPS)), dim3(POLICY_WARPS * 32), 0, s,
                                      A, D);
-        const int spans = (C + POLICY_BACK_SPAN - 1) / POLICY_BACK_SPAN;
+        const int spans = (int)parts_of(C, POLICY_BACK_SPAN);
         return launch_overlapped(policy_backward_long_kernel<B, R, I>, dim3((unsigned)((int64_t)nq * spans)), dim3(POLICY_BACK_THREADS), 0, s, A, D, spans);
     }), 1, "policy loss backward kernel");
 }

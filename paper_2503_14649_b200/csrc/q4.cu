@@ -590,8 +590,8 @@ __global__ void __launch_bounds__(Q4B_THREADS, 2) q4_rescore_backward_kernel(con
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = f2(0.f, 0.f);
     const int grp = part * 16 / R.group;
-    for (int base = j0; base < j1; base += Q4B_STAGE) {
-        const int n = min(Q4B_STAGE, j1 - base);
+    for (int64_t base = j0; base < j1; base += Q4B_STAGE) {  // k may be the largest int
+        const int n = (int)min((int64_t)Q4B_STAGE, j1 - base);
         __syncthreads();
         int have = 0;
         for (int i0 = 0; i0 < n; i0 += threads) {  // keep the candidates that are there, in their order
@@ -758,8 +758,7 @@ static Q4ScoresPlan q4_scores_plan(const Q4Rows& R, bool bf16, int nq, int sms) 
     int most = P.mode == Q4_F32_PACKED ? 1 : (int)(room / (parts * tile));
     if (most > (bf16 ? Q4S_MAX_TILES : 4)) most = bf16 ? Q4S_MAX_TILES : 4;
     if (most == 7) most = 6;
-    P.tiles = (nq + per_tile - 1) / per_tile;
-    if (P.tiles > most) P.tiles = most;
+    P.tiles = (int)min((int64_t)most, parts_of(nq, per_tile));
     if (P.tiles == 7) P.tiles = 8;  // not built
     P.nq = nq < P.tiles * per_tile ? nq : P.tiles * per_tile;
     const size_t x = tile * P.tiles * parts;
@@ -877,8 +876,8 @@ extern "C" rago_status rago_q4_rescore(const uint8_t* codes, const void* scales,
         constexpr bool Q = decltype(qb)::value, S = decltype(sb)::value, L = decltype(l2)::value;
         auto launch = [&](auto kernel, int lanes) {
             // CTAs per query: enough to fill the GPU a few times over, each warp with something to do
-            const int turns = (k + 64 / lanes - 1) / (64 / lanes), most = (turns + Q4R_WARPS - 1) / Q4R_WARPS;
-            int64_t per = (8LL * sms + nq - 1) / nq;
+            const int64_t most = parts_of(parts_of(k, 64 / lanes), Q4R_WARPS);
+            int64_t per = parts_of(8LL * sms, nq);
             per = per < most ? per : most;
             return launch_overlapped(kernel, dim3((unsigned)nq, (unsigned)(per < 65535 ? per : 65535)), dim3(Q4R_WARPS * 32), (size_t)d * 4, s, R, queries, ids, k, out_dists);
         };
