@@ -465,7 +465,7 @@ rago_status rago_list_balance(const void* logits, rago_dtype dtype, int32_t nq, 
 
 /*
  * Its backward pass (counts are constants): grad_logits_l = grad_loss * nlist / n * scale * p_l (f_l - sum_m f_m p_m) in counted
- * rows, 0 in the others.
+ * rows, 0 in the others.  What all f have in common goes out exactly: even lists have no gradient, nearly even ones keep theirs.
  *   counts, stats  as the forward pass left them;  grad_loss  dev fp32 [1]
  *   grad_logits    dev [nq][nlist], the type of the logits; may not overlap an input
  */

@@ -2,9 +2,9 @@
 //
 // loss = nlist / n * sum_rows sum_l f_l p_l with f_l = counts_l / T: given the counts, a row needs one pass for some logit m near
 // its best, Z = sum 2^t_l and D = sum counts_l 2^t_l (t_l = (logit_l - m) a, a = scale * log2 e; the difference comes first, so logits may be
-// of any size, masked with the type's lowest value among them); the mean of p over the batch is never formed.  Where lists are few
-// their smallest count is taken off all of them first, exactly: what the gradient is made of, f_l less the row's sum f p, is then not
-// lost where lists are nearly even, and 0 where they are.  The backward pass reads the logits once more and writes the gradient.
+// of any size, masked with the type's lowest value among them); the mean of p over the batch is never formed.  The smallest count
+// is taken off all counts first, exactly: what the gradient is made of, f_l less the row's sum f p, is then not lost where lists are
+// nearly even, and 0 where they are.  The backward pass reads the logits once more and writes the gradient.
 //
 // Measured: 4096 rows of 65 536 bf16 logits, forward 123 us (4.4 TB/s; exponentials and the ten instructions around them) and backward
 // 175 (6.1 TB/s); 1021 rows of 4096 fp32 logits 14 and 5.7.
@@ -38,6 +38,8 @@ __device__ __forceinline__ float balance_exp2(float x) {
 // that takes 2.4 us longer on the GPU than clearing and adding, which is captured calls' loss, and saves a launch of 4 us on the host, which
 // bounds such calls otherwise; at 6400 slots of 65 536 lists it is 3 us faster on the GPU too.)  More slots are dealt out to CTAs, which add what they
 // counted (in shared memory where the lists fit, so that few lists are not contended for) to counts that were cleared before.
+constexpr int BALANCE_SHORT_LISTS = 1024;  // rows of up to as many are short: part of a warp each, or a warp
+constexpr int BALANCE_OWN_LEAST = 4096;
 constexpr int BALANCE_SHARED_LISTS = 8192, BALANCE_RANGE_SLOTS = 1 << 15, BALANCE_RANGE_LISTS = 1024, BALANCE_RANGE_CTAS = 64, BALANCE_COUNT_THREADS = 512;
 
 // Lists l0 .. l0 + range - 1 per CTA; the first one also counts slots and rows
@@ -93,10 +95,38 @@ __global__ void __launch_bounds__(BALANCE_THREADS) balance_clear_kernel(int32_t*
     grid_dependents_may_launch();
     const int i = blockIdx.x * BALANCE_THREADS + threadIdx.x;
     if (i < nlist) counts[i] = 0;
-    if (i == 0) { totals->rows = totals->slots = 0u; *ticket = 0u; }
+    if (i == 0) { totals->rows = totals->slots = 0u; *ticket = 0u; totals->per_slot = __int_as_float(0); }
 }
 
-// SHARED: count in shared memory
+// The smallest count, where the word that 1 / T goes to in the end holds it (volatile: read once, before the last CTA overwrites it)
+__device__ __forceinline__ int balance_kept(const BalanceTotals* totals) { return __float_as_int(*const_cast<const volatile float*>(&totals->per_slot)); }
+// The smallest of all counts, by a CTA.  Where there are fewer slots than lists it is 0 (looked at where that saves reading many counts:
+// the slots would be waited for), and a thread that has met a 0 is done.
+template <int THREADS>
+__device__ __forceinline__ int balance_least(const int32_t* counts, int nlist, uint32_t T) {
+    __shared__ int least;
+    if (nlist > BALANCE_SHARED_LISTS && T < (uint32_t)nlist) return 0;
+    if (threadIdx.x == 0) least = 0x7fffffff;
+    __syncthreads();
+    int base = 0x7fffffff;
+    const int whole = (reinterpret_cast<uintptr_t>(counts) & 15) == 0 ? nlist / 4 : 0;  // in fours
+    for (int l = threadIdx.x; l < whole && base; l += 8 * THREADS) {
+        int4 c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = reinterpret_cast<const int4*>(counts)[min(l + i * THREADS, whole - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) base = min(min(base, min(c[i].x, c[i].y)), min(c[i].z, c[i].w));
+    }
+    for (int64_t l = 4 * whole + threadIdx.x; l < nlist && base; l += THREADS) base = min(base, counts[l]);
+    base = __reduce_min_sync(0xffffffffu, base);
+    if ((threadIdx.x & 31) == 0) atomicMin(&least, base);
+    __syncthreads();
+    return least;
+}
+
+// SHARED: count in shared memory.  Up to BALANCE_OWN_LEAST counts, which 128 threads read in one go, the rows' CTAs find the smallest
+// themselves (0.8 us at 1021 rows of 4096 lists, 2.3 by the last CTA here); of more the last CTA here does (2.2 us at 4096 rows of
+// 8192 lists, 4.9 by the rows' CTAs).
 template <bool SHARED>
 __global__ void __launch_bounds__(BALANCE_COUNT_THREADS) balance_count_kernel(const int32_t* __restrict__ lists, const uint8_t* __restrict__ valid, int nq,
                                                                               int nprobe, int nlist, int32_t* __restrict__ counts, BalanceTotals* __restrict__ totals) {
@@ -133,6 +163,17 @@ __global__ void __launch_bounds__(BALANCE_COUNT_THREADS) balance_count_kernel(co
     if (SHARED)
         for (int l = tid; l < nlist; l += BALANCE_COUNT_THREADS)
             if (here[l]) atomicAdd(&counts[l], here[l]);
+    if (nlist <= BALANCE_OWN_LEAST) return;
+    // the word of 1 / T counts the CTAs that are done, and holds the smallest count from then on until the rows are done
+    __shared__ bool last;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) last = atomicAdd(reinterpret_cast<uint32_t*>(&totals->per_slot), 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    const int base = balance_least<BALANCE_COUNT_THREADS>(counts, nlist, __ldcg(&totals->slots));
+    if (tid == 0) totals->per_slot = __int_as_float(base);
 }
 
 // ---- rows --------------------------------------------------------------------------------------------------------------------
@@ -374,7 +415,7 @@ __global__ void __launch_bounds__(BALANCE_THREADS) balance_short_rows_kernel(con
 // them (WHOLE: rows and counts of whole 16-byte pieces), or are at least met again in L1.
 template <bool BF16, int ROWS, bool WHOLE, int THREADS>
 __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balance_rows_kernel(const void* __restrict__ logits, int nq, int nlist, float a, const uint8_t* __restrict__ valid,
-                                                               const int32_t* __restrict__ counts, BalanceTotals* __restrict__ totals,
+                                                               const int32_t* __restrict__ counts, bool has_base, BalanceTotals* __restrict__ totals,
                                                                uint32_t* __restrict__ ticket, float4* __restrict__ stats, float* __restrict__ loss) {
     using P = LogitPiece<BF16>;
     __shared__ BalanceSums part[THREADS / 32][ROWS];
@@ -383,7 +424,8 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
     grid_dependents_may_launch();
     const int q0 = blockIdx.x * ROWS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t T = totals->slots;
-    constexpr int base = 0;
+    int base = 0;
+    if (has_base) base = balance_kept(totals);
     BalanceSums S[ROWS];
     bool counted[ROWS];
 #pragma unroll
@@ -392,8 +434,10 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
         counted[r] = q0 + r < nq && (!valid || valid[q0 + r]);
     }
     if (ROWS == 1) {
+        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
         if (counted[0]) balance_sweep<BF16>(S[0], logits, (size_t)q0 * nlist, nlist, a, counts, base, tid, THREADS);
     } else if (!WHOLE) {
+        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
         int head[ROWS], pieces[ROWS], most = 0;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -432,6 +476,7 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
                 if (counted[r] && l < nlist) next[r] = P::load(logits, (size_t)(q0 + r) * nlist + l);
         };
         fetch(tid * P::UNIT);
+        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
         for (int l = tid * P::UNIT; l < nlist; l += THREADS * P::UNIT) {
             uint4 w[ROWS];
 #pragma unroll
@@ -690,7 +735,9 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
     ranges = ranges < BALANCE_RANGE_CTAS ? ranges : BALANCE_RANGE_CTAS;
     const int range = (int)parts_of(nlist, ranges);
     cudaError_t e;
-    if (slots <= BALANCE_RANGE_SLOTS && range <= BALANCE_SHARED_LISTS) {
+    const bool ranges_do = slots <= BALANCE_RANGE_SLOTS && range <= BALANCE_SHARED_LISTS;
+    const bool has_base = !ranges_do && nlist > BALANCE_OWN_LEAST;  // the smallest count is known before the rows
+    if (ranges_do) {
         e = launch_overlapped(balance_count_ranges_kernel, dim3((unsigned)parts_of(nlist, range)), dim3(BALANCE_RANGE_THREADS), (size_t)range * 4, s, lists, valid,
                               nq, nprobe, nlist, range, out_counts, totals, ticket);
         ++launches;
@@ -712,11 +759,15 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
         auto rows = [&](auto bf16) {
             constexpr bool B = decltype(bf16)::value;
             auto launch = [&](auto kernel, int per_cta, int threads) {
-                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts,
+                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts, has_base,
                                          totals, ticket, stats, out_loss);
             };
-            if (nlist <= (B ? 128 : 64)) return launch(balance_short_rows_kernel<B, 8, 1>, 32, BALANCE_THREADS);
-            if (nlist <= 1024) return nq >= 8192 ? launch(balance_short_rows_kernel<B, 32, 2>, 16, BALANCE_THREADS) : launch(balance_short_rows_kernel<B, 32, 1>, 8, BALANCE_THREADS);
+            auto launch_short = [&](auto kernel, int per_cta) {
+                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3(BALANCE_THREADS), 0, s, logits, nq, nlist, a, valid, out_counts, totals, ticket,
+                                         stats, out_loss);
+            };
+            if (nlist <= (B ? 128 : 64)) return launch_short(balance_short_rows_kernel<B, 8, 1>, 32);
+            if (nlist <= BALANCE_SHORT_LISTS) return nq >= 8192 ? launch_short(balance_short_rows_kernel<B, 32, 2>, 16) : launch_short(balance_short_rows_kernel<B, 32, 1>, 8);
             if (nq >= 2048) return whole ? launch(balance_rows_kernel<B, 4, true, 128>, 4, 128) : launch(balance_rows_kernel<B, 4, false, 128>, 4, 128);
             if (nq >= 1024) return whole ? launch(balance_rows_kernel<B, 2, true, 128>, 2, 128) : launch(balance_rows_kernel<B, 2, false, 128>, 2, 128);
             if (nq >= 512) return launch(balance_rows_kernel<B, 1, false, 128>, 1, 128);
