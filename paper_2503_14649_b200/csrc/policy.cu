@@ -23,8 +23,7 @@ struct PolicyArgs {
     const void *scores, *ref;
     const int64_t* ids;
     int nq, C, G;
-    float a;       // scale * log2 e
-    float unit;    // the sign of a times 2^-24: unit * score is larger for better candidates, and sums of differences of the type's
+    float unit;    // the sign of a = scale * log2 e times 2^-24: unit * score is larger for better candidates, and sums of differences of the type's
                    // lowest values stay finite
     float step;    // |a| * 2^24, so that unit * step = a
     float scale;
@@ -165,7 +164,7 @@ __device__ __forceinline__ bool policy_sample(const PolicyArgs& A, const PolicyR
     const size_t at = (size_t)q * A.C + c;
     const float s = load_s<BF16>(A.scores, at);
     if (!policy_there(A, at, s)) return false;
-    *logp = LN2 * fmaf(s - r.m, A.a, -r.lz);
+    *logp = LN2 * fmaf(fmaf(s, A.unit, -r.m * A.unit), A.step, -r.lz);
     return true;
 }
 
@@ -376,7 +375,7 @@ struct PolicyGrads {
 };
 // What is the same for all candidates of a row: the gradient is pi (by_gap * (log2 pi - log2 rho) + flat), and by_own * own more where
 // samples chose the candidate.
-struct PolicyBack { PolicyRow r; float a, lowest, by_gap, flat, by_own; };
+struct PolicyBack { PolicyRow r; float unit, step, lowest, by_gap, flat, by_own; };  // r.m and r.mr times unit
 
 // Slope of sample t by log pi, and the candidate it belongs to (-1: does not count)
 __device__ __forceinline__ float policy_slope(const PolicyArgs& A, const PolicyGrads& D, int q, int t, int* to) {
@@ -394,8 +393,9 @@ __device__ __forceinline__ float policy_slope(const PolicyArgs& A, const PolicyG
 
 template <bool REF>
 __device__ __forceinline__ float policy_grad(const PolicyBack& B, float score, float ref) {
-    const float l = fmaf(score - B.r.m, B.a, -B.r.lz), p = exp2_fast(l);
-    const float g = p * (REF ? fmaf(B.by_gap, l - fmaf(ref - B.r.mr, B.a, -B.r.lzr), B.flat) : B.flat);
+    // unit * score - unit * best in one rounding: a difference of scores of any size
+    const float l = fmaf(fmaf(score, B.unit, -B.r.m), B.step, -B.r.lz), p = exp2_fast(l);
+    const float g = p * (REF ? fmaf(B.by_gap, l - fmaf(fmaf(ref, B.unit, -B.r.mr), B.step, -B.r.lzr), B.flat) : B.flat);
     return p == 0.f ? 0.f : g;  // a missing candidate, or one next to impossible: whatever its reference is
 }
 
@@ -403,7 +403,7 @@ template <bool REF>
 __device__ __forceinline__ PolicyBack policy_back(const PolicyArgs& A, const PolicyGrads& D, int q, float H) {
     const float4 st = D.stats[q];
     const float gp = A.G ? D.grad_policy[q] : 0.f, gk = REF ? D.grad_kl[q] : 0.f;
-    return {{st.x, st.y, st.z, st.w}, A.a, A.lowest, A.scale * gk * LN2, -A.scale * (gp * H + (REF ? gk * D.kl[q] : 0.f)), A.scale * gp};
+    return {{st.x * A.unit, st.y, st.z * A.unit, st.w}, A.unit, A.step, A.lowest, A.scale * gk * LN2, -A.scale * (gp * H + (REF ? gk * D.kl[q] : 0.f)), A.scale * gp};
 }
 
 // one candidate, own: the slopes of the samples that chose it
@@ -537,9 +537,10 @@ static rago_status policy_check(const void* scores, const void* ref, rago_dtype 
     if (policy_off(chosen) || policy_off(old_logp) || policy_off(advantage)) return policy_fail(RAGO_EALIGN, "chosen, old_logp or advantage are not aligned to their type");
     A->scores = scores; A->ref = ref; A->ids = ids; A->lowest = scale > 0.f ? -INFINITY : INFINITY; A->unit = scale > 0.f ? 0x1p-24f : -0x1p-24f;
     A->nq = nq; A->C = C; A->G = G;
-    A->a = (float)((double)scale * 1.44269504088896340736); A->scale = scale;
-    A->step = fabsf(A->a) * 0x1p24f;
-    if (A->a == 0.f) return policy_fail(RAGO_EINVAL, "scale must be finite and not 0");
+    const float a = (float)((double)scale * 1.44269504088896340736);
+    A->scale = scale;
+    A->step = fabsf(a) * 0x1p24f;
+    if (a == 0.f) return policy_fail(RAGO_EINVAL, "scale must be finite and not 0");
     if (!(A->step - A->step == 0.f)) return policy_fail(RAGO_EUNSUPPORTED, "scale exceeds 1e31 in magnitude");
     A->chosen = chosen; A->old_logp = old_logp; A->advantage = advantage;
     A->low = 1.f - clip_low; A->high = 1.f + clip_high;
