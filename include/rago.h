@@ -451,7 +451,7 @@ rago_status rago_policy_loss_backward(const void* scores, const void* ref_scores
  *     loss     = nlist / n * sum_rows sum_l f_l p_l        (1 for even lists or an even p)
  *   logits     dev [nq][nlist], RAGO_F32 or RAGO_BF16: the coarse scores; -infinity after scaling is p = 0.  A row without a finite
  *              one, and all of its slots, count in n, T and counts, and add nothing to the loss
- *   scale      finite, not 0: 1 / temperature, negative for distances
+ *   scale      finite, at least 1e-36 in magnitude: 1 / temperature, negative for distances
  *   lists      dev int32 [nq][nprobe] as rago_search_probes leaves them; a number outside 0 .. nlist - 1 is not counted
  *   valid      dev uint8 [nq] or NULL: rows with 0 are padding and are not looked at
  *   out_loss   dev fp32 [1];  out_counts  dev int32 [nlist]

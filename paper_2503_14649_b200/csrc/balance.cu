@@ -696,6 +696,9 @@ static rago_status balance_check(const void* logits, rago_dtype dtype, int32_t n
     *a = (float)((double)scale * 1.44269504088896340736);
     if (!(scale - scale == 0.f) || scale == 0.f || !(*a - *a == 0.f) || *a == 0.f)
         return balance_fail(RAGO_EINVAL, "scale must be finite and not 0");
+    // a difference of logits that leaves fp32 is a weight of 0 for every larger scale (units of their own for logits, as the policy's
+    // scores have, took 4096 x 65 536 from 328 to 337 us)
+    if (fabsf(scale) < 1e-36f) return balance_fail(RAGO_EUNSUPPORTED, "scale is below 1e-36 in magnitude");
     if (nq > 0 && !logits) return balance_fail(RAGO_EINVAL, "logits are null");
     if ((long long)nq * nlist >= (1LL << 40)) return balance_fail(RAGO_EUNSUPPORTED, "nq * nlist = %lld is 2^40 or more", (long long)nq * nlist);
     if (reinterpret_cast<uintptr_t>(logits) % (dtype == RAGO_F32 ? 4 : 2)) return balance_fail(RAGO_EALIGN, "logits are not aligned to their type");

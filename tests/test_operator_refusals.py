@@ -122,6 +122,12 @@ def test_list_balance(status, changes):
     assert call("rago_list_balance_backward", BALANCE_BACKWARD, **changes) == status
 
 
+@pytest.mark.parametrize("scale", [9e-37, -9e-37, 1e-44])
+def test_list_balance_scales_that_would_lose_differences_of_logits(scale):
+    assert call("rago_list_balance", BALANCE, scale=scale) == EUNSUPPORTED
+    assert call("rago_list_balance_backward", BALANCE_BACKWARD, scale=scale) == EUNSUPPORTED
+
+
 def test_list_balance_inputs_and_outputs():
     assert call("rago_list_balance", BALANCE, nprobe=0) == EINVAL
     assert call("rago_list_balance", BALANCE, lists=None) == EINVAL
