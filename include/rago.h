@@ -378,6 +378,8 @@ rago_status rago_q4_scores(const uint8_t* codes, const void* scales, rago_dtype 
  *   ids        dev int64 [nq][k]: row numbers.  An id outside 0 .. N - 1, a search's padding -1 among them, is a missing
  *              candidate: its distance is +INFINITY (L2) or -INFINITY (IP).  The same id may appear twice.
  *   out_dists  dev fp32 [nq][k], in the order of ids (rago_merge_results with nparts = 1 puts them best first)
+ * An inner product sums 32 products of query numbers and codes before their scale: it holds query numbers of up to 2^119 (6e35) in
+ * magnitude with any scales; larger ones may come out infinite where scaled products would not.
  * nq * k < 2^31.
  */
 rago_status rago_q4_rescore(const uint8_t* codes, const void* scales, rago_dtype scale_dtype, int64_t N, int32_t d,

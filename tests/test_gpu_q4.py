@@ -262,6 +262,18 @@ def test_a_query_that_is_a_stored_row_has_distance_zero():
 
 
 @pytest.mark.parametrize("query", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 160, 768])
+def test_candidates_hold_queries_and_scales_of_any_size(d, query):
+    """Query numbers up to 2^119 with small scales, and scales up to 1e32 with small queries: the scaled products are ordinary ones."""
+    for scale, size in ((1e-30, 2.0 ** 116), (1e34, 1e-30)):
+        codes, scales = make_rows(400, d, 32, torch.float32)
+        scales *= scale
+        q = (make_queries(3, d, torch.float32).clamp(-8, 8) * size).to(DTYPES[query])
+        check_candidates(codes, scales, q, make_ids(3, 30, 400), 32, "ip", torch.randn((3, 30), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda"))
+        check_scores(codes, scales, q, 32)
+
+
+@pytest.mark.parametrize("query", ["f32", "bf16"])
 @pytest.mark.parametrize("near", [1.0, 0.01, 1e-3])
 @pytest.mark.parametrize("nq,k,d", [(1, 700, 96), (5, 33, 160), (300, 100, 768), (2, 9, 8192)])
 def test_the_gradient_of_near_candidates(nq, k, d, near, query):
