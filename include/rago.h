@@ -365,8 +365,10 @@ rago_status rago_merge_results(const int64_t* part_ids, const float* part_dists,
  *   out_scores  dev fp32 [nq][N]
  * nq == 0 and N == 0 are no-ops.  Made for few queries: rows of up to 1024 numbers are read once for every 64 bf16 or 32 fp32
  * queries, longer rows once for every 65 536 / d or 32 768 / d of them (d rounded up to a power of two).
- * A query's numbers enter with an error of at most 2^-24 of themselves, or 2^-39 of the query's largest where that is more
- * (numbers less than 2^-15 of the largest: an fp32 number keeps fewer bits there, a bf16 number is exact down to 2^-31 of it).
+ * An fp32 query's numbers enter with an error of at most 2^-23 of themselves, or 2^-39 of the query's largest where that is more
+ * (numbers less than 2^-16 of the largest); a bf16 query's are exact down to 2^-31 of the largest.
+ * Sums are taken in the same order from call to call.  That order goes by N and nq too, so the last bits of a row's score may change
+ * when the store grows, or differ between a store and a part of it.
  */
 rago_status rago_q4_scores(const uint8_t* codes, const void* scales, rago_dtype scale_dtype, int64_t N, int32_t d,
                            int32_t group, const void* queries, rago_dtype query_dtype, int32_t nq, float* out_scores,

@@ -26,13 +26,15 @@ __device__ __forceinline__ float load_f(const void* base, size_t i) {
     return static_cast<const float*>(base)[i];
 }
 // ---- scores of every row -----------------------------------------------------------------------------------------------
-// 2 nq N d operations on N d / 2 bytes: for few queries the rows' bytes bound it, so the work per byte has to be small.  c - 8 is exact in
-// fp16 and costs 1.1 instructions a number: nibbles i and i + 4 of a word are masked into the mantissas of two 1024s at a time (16 c
-// in place of c for every second pair, which saves the shift), one fp16 instruction takes the rest off.  The matrix instruction
-// (m16n8k16, 16 rows by 8 queries, fp32 sums) does the products.
+// 2 nq N d operations on N d / 2 bytes: for few queries the rows' bytes bound it, so the work per byte has to be small.  A small number
+// put into the mantissa of a power of two that is then taken off is a published way around conversions (Kim, Henry, Fahim and Hassan
+// Awadalla, "Who Says Elephants Can't Run", 2022, for 4 and 8 bits and fp16); here c - 8, exact in fp16, costs 1.1 instructions a number:
+// nibbles i and i + 4 of a word are masked into the mantissas of two 1024s at a time (16 c in place of c for every second pair, which
+// saves the shift), one fp16 instruction takes the rest off.  The matrix instruction (m16n8k16, 16 rows by 8 queries, fp32 sums) does
+// the products.
 // Queries go in as fp16 after a power of two per query that brings its largest number to 2^14 .. 2^15 (taken off the sums again):
-// a bf16 number fits as it is, an fp32 number is cut into two parts, hi = fp16(x) and fp16(x - hi), off by at most half a step of
-// fp32.  What lies 2^15 and more below the query's largest number is off by at most 2^-39 of that number instead.  The parts'
+// a bf16 number fits as it is, an fp32 number is cut into two parts, hi = fp16(x) and fp16(x - hi), 23 of its 24 bits: off by at
+// most 2^-23 of itself, or by 2^-39 of the query's largest number where that is more.  The parts'
 // products add up in the same fp32 accumulators; up to four fp32 queries put their parts side by side into the eight columns, so that
 // one instruction does for all of them.  The sum over a group is multiplied by the row's scale and added to the row's total.
 //

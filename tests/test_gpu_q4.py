@@ -88,6 +88,27 @@ def test_scores_hold_queries_of_any_size():
     check_scores(codes, scales, q, 64)
 
 
+@pytest.mark.parametrize("nq", [3, 12])
+@pytest.mark.parametrize("query", ["f32", "bf16"])
+def test_a_querys_numbers_enter_with_the_error_that_the_header_states(nq, query):
+    """Rows that are 1 in one place and 0 elsewhere: the score is that number of the query, no sum rounds it."""
+    d = 256
+    codes = torch.full((d, d // 2), 0x88, dtype=torch.uint8, device="cuda")
+    i = torch.arange(d, device="cuda")
+    codes[i, i // 2] = torch.where(i % 2 == 0, 0x89, 0x98).to(torch.uint8)
+    scales = torch.ones((d, d // 32), device="cuda")
+    q = make_queries(nq, d, torch.float32)
+    q[0] *= 2.0 ** torch.linspace(0, -40, d, device="cuda")
+    q[1, :4] = torch.tensor([1 + 2 ** -11 - 2 ** -23, -1 - 2 ** -11 + 2 ** -23, 1 + 3 * 2 ** -23, 2 - 2 ** -23], device="cuda")
+    q = q.to(DTYPES[query])
+    got, x = binding.rago_q4_scores(codes, scales, q, 32).double(), q.double()
+    top = x.abs().amax(1, keepdim=True)
+    if query == "bf16":
+        exact = x.abs() >= 2.0 ** -31 * top
+        assert (got == x)[exact].all()
+    assert ((got - x).abs() <= torch.maximum(2.0 ** -23 * x.abs(), 2.0 ** -39 * top)).all()
+
+
 @pytest.mark.parametrize("nq,query", [(1, "f32"), (4, "f32"), (20, "f32"), (3, "bf16"), (40, "bf16")])
 @pytest.mark.parametrize("scale,group", [("f32", 32), ("bf16", 128)])
 def test_scores_hold_scales_of_any_size(nq, query, scale, group):
