@@ -88,6 +88,22 @@ def test_scores_hold_queries_of_any_size():
     check_scores(codes, scales, q, 64)
 
 
+@pytest.mark.parametrize("d,group,scale", [(416, 32, "bf16"), (416, 128, "f32"), (768, 32, "f32"), (768, 64, "bf16"), (768, 128, "f32"), (2048, 64, "f32")])
+@pytest.mark.parametrize("query", ["f32", "bf16"])
+@pytest.mark.parametrize("nq", [1, 5, 12, 20, 37, 64])
+def test_scores_of_more_rows_than_one_tile_a_warp(nq, query, d, group, scale):
+    """Several tiles of rows a warp (3126 and more for 1776 or 2368 warps, or half as many teams of two), with any number of tiles of columns and
+    any group: rings, scales and shared sums are carried from tile to tile.  Every score is looked at."""
+    for N in ((100_003,) if d > 768 else (100_003, 133_337)):
+        codes, scales = make_rows(N, d, group, DTYPES[scale])
+        q = make_queries(nq, d, DTYPES[query])
+        got, x = binding.rago_q4_scores(codes, scales, q, group), q.double()
+        for r in range(0, N, 20_000):
+            w = values64(codes[r:r + 20_000], scales[r:r + 20_000], group)
+            tol = SECOND_ORDER * (d + 4) * U * (x.abs() @ w.abs().T)
+            assert ((got[:, r:r + 20_000].double() - x @ w.T).abs() <= tol).all(), (N, r)
+
+
 @pytest.mark.parametrize("nq", [3, 12])
 @pytest.mark.parametrize("query", ["f32", "bf16"])
 def test_a_querys_numbers_enter_with_the_error_that_the_header_states(nq, query):
@@ -255,6 +271,30 @@ def test_candidates_for_any_batch(nq, k):
     codes, scales = make_rows(1000, 96, 32, torch.bfloat16)
     grad = torch.randn((nq, k), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
     check_candidates(codes, scales, make_queries(nq, 96, torch.float32), make_ids(nq, k, 1000), 32, "l2", grad)
+
+
+@pytest.mark.parametrize("metric", ["l2", "ip"])
+@pytest.mark.parametrize("query", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,k,d", [(300, 513, 64), (297, 1300, 96), (40, 5000, 32), (1, 9001, 160), (2, 4097, 8192), (300, 1025, 16 * 26)])
+def test_more_candidates_than_a_cta_stages_at_a_time(nq, k, d, query, metric):
+    """Over 512 a CTA, alone or in a cluster, with stretches of missing ones of any length."""
+    codes, scales = make_rows(1000, d, 32, torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    ids = make_ids(nq, k, 1000)
+    ids[nq // 2, 100:100 + k // 2] = -1
+    ids[:, ::7] = -1
+    grad = torch.randn((nq, k), generator=g, device="cuda")
+    x = make_queries(nq, d, DTYPES[query])
+    got = binding.rago_q4_rescore_backward(codes, scales, x, ids, 32, metric, grad).double()
+    w = values64(codes, scales, 32)
+    for r in range(nq):
+        there = (ids[r] >= 0) & (ids[r] < 1000)
+        rows = w[ids[r][there]]
+        terms = grad[r][there].double()[:, None] * (2 * (x[r].double() - rows) if metric == "l2" else rows)
+        tol = SECOND_ORDER * (k + 6) * U * terms.abs().sum(0)
+        if query == "bf16":
+            tol = tol + 2.0 ** -8 * terms.sum(0).abs() + 1e-38
+        assert ((got[r] - terms.sum(0)).abs() <= tol).all(), r
 
 
 def test_a_query_without_candidates_and_bad_gradients_of_missing_ones():
