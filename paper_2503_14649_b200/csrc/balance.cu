@@ -769,10 +769,20 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
                 return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3(BALANCE_THREADS), 0, s, logits, nq, nlist, a, valid, out_counts, totals, ticket,
                                          stats, out_loss);
             };
+            // What a row is given, each rule with the forward pass's us on its two sides (in a stream of such passes, rows x lists, fp32 unless bf16 is said):
+            // up to 16 pieces 8 lanes: 16 384 x 64 10.8, a warp 16.8; 16 384 x 128 bf16 11.7 and 19.1
             if (nlist <= (B ? 128 : 64)) return launch_short(balance_short_rows_kernel<B, 8, 1>, 32);
+            // up to 1024 lists a warp: 1000 x 512 9.3, a CTA 10.7; 8192 x 1024 21.4 and 23.5, but 1000 x 1024 12.0 and 10.4, 8192 x 2048 31.6 and
+            // 29.1 (64 rows would take a CTA each from 512 lists on: 9.2 and 6.5); two rows a warp from 8192 rows: 8192 x 512 16.6, one 19.2, but
+            // 4096 x 512 13.6 and 11.9
             if (nlist <= BALANCE_SHORT_LISTS) return nq >= 8192 ? launch_short(balance_short_rows_kernel<B, 32, 2>, 16) : launch_short(balance_short_rows_kernel<B, 32, 1>, 8);
-            if (nq >= 2048) return whole ? launch(balance_rows_kernel<B, 4, true, 128>, 4, 128) : launch(balance_rows_kernel<B, 4, false, 128>, 4, 128);
+            // four rows a CTA of 128 threads where that fills the GPU: 16 384 x 4096 bf16 56, two 63; 4096 x 65 536 185 and 210 (in bf16 129 and 123), but
+            // 2048 x 65 536 bf16 94 and 73, 2048 x 4095 23.3 and 18.2
+            if (nq >= 4096) return whole ? launch(balance_rows_kernel<B, 4, true, 128>, 4, 128) : launch(balance_rows_kernel<B, 4, false, 128>, 4, 128);
+            // two: 1024 x 65 536 bf16 51.5, one 54.0; 2048 x 4096 15.5 and 22.2
             if (nq >= 1024) return whole ? launch(balance_rows_kernel<B, 2, true, 128>, 2, 128) : launch(balance_rows_kernel<B, 2, false, 128>, 2, 128);
+            // one: 600 x 8192 17.6, with 256 threads 18.7; fewer rows with 256: 300 x 4096 8.6, with 128 10.8, with 512 11.0; longer ones with 512:
+            // 128 x 32 768 bf16 11.4, with 256 15.6
             if (nq >= 512) return launch(balance_rows_kernel<B, 1, false, 128>, 1, 128);
             return nlist >= 16384 ? launch(balance_rows_kernel<B, 1, false, 512>, 1, 512) : launch(balance_rows_kernel<B, 1, false, 256>, 1, 256);
         };

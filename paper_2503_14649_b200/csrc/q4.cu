@@ -47,7 +47,10 @@ __device__ __forceinline__ float load_f(const void* base, size_t i) {
 // (groups of 32) for 37 queries 255 us, where each group's 80 sums a lane are scaled between the matrix instructions.
 constexpr int Q4S_ROWS = 32, Q4S_STRIDE = 80;  // 64 bytes of a row a stage, spaced 20 words: the 8 rows of a fragment meet no bank twice
 constexpr int Q4S_STAGE = Q4S_ROWS * Q4S_STRIDE;
-constexpr int Q4S_SPLIT_TILES = 2;  // most tiles of columns for which warps may share a tile of rows
+// Most tiles of columns (times parts) for which warps may share a tile of rows.  (1000 rows of 768 for one query 4.1 us, not shared 4.9; three and four
+// tiles gain less, 1000 rows for 20 bf16 queries 6.2 instead of 7.3 and nothing at 100 000, for as many kernels more.)  Kernels of 8
+// warps are built for as many tiles, and the plan asks for them with up to two.
+constexpr int Q4S_SPLIT_TILES = 2;
 constexpr int Q4S_MAX_TILES = 8, Q4S_MAX_NQ = 8 * Q4S_MAX_TILES;  // eight queries a tile
 
 enum { Q4_BF16 = 0, Q4_F32 = 1, Q4_F32_PACKED = 2 };  // how queries go in; parts side by side in the tiles' order: 1, 2, 1
@@ -766,6 +769,7 @@ static Q4ScoresPlan q4_scores_plan(const Q4Rows& R, bool bf16, int nq, int sms) 
     if (P.tiles == 7) P.tiles = 8;  // not built
     P.nq = nq < P.tiles * per_tile ? nq : P.tiles * per_tile;
     const size_t x = tile * P.tiles * parts;
+    static_assert(Q4S_SPLIT_TILES >= 2, "kernels of 8 warps are built up to there");
     const bool two = P.tiles * parts <= 2 && q4s_ring(8, 4) + x <= Q4S_SMEM_TWO;
     P.warps = two ? 8 : 12;
     P.per_sm = two ? 2 : 1;
@@ -879,13 +883,15 @@ extern "C" rago_status rago_q4_rescore(const uint8_t* codes, const void* scales,
     e = q4_types(query_dtype, scale_dtype, metric, [&](auto qb, auto sb, auto l2) {
         constexpr bool Q = decltype(qb)::value, S = decltype(sb)::value, L = decltype(l2)::value;
         auto launch = [&](auto kernel, int lanes) {
-            // CTAs per query: enough to fill the GPU a few times over, each warp with something to do
+            // CTAs per query: enough to fill the GPU a few times over, each warp with something to do (1024 x 100 of 768: 19.1 us, 2 CTAs an
+            // SM 21.5, 32 18.6)
             const int64_t most = parts_of(parts_of(k, 64 / lanes), Q4R_WARPS);
             int64_t per = parts_of(8LL * sms, nq);
             per = per < most ? per : most;
             return launch_overlapped(kernel, dim3((unsigned)nq, (unsigned)(per < 65535 ? per : 65535)), dim3(Q4R_WARPS * 32), (size_t)d * 4, s, R, queries, ids, k, out_dists);
         };
-        // rows of up to 128 numbers are four lanes' work at most
+        // rows of up to 128 numbers are four lanes' work at most: 4096 x 100 of 128 16.1 us, with 8 lanes 27.0 (few candidates go the other way, 64 x 20
+        // 2.0 and 1.8; of 256 numbers 27.5 and 28.6, 64 x 20 2.9 and 1.6)
         return d <= 128 ? launch(q4_rescore_kernel<Q, S, L, 2>, 2) : launch(q4_rescore_kernel<Q, S, L, 8>, 8);
     });
     return q4_done(e, 1, "4-bit rescore kernel");
@@ -905,6 +911,9 @@ extern "C" rago_status rago_q4_rescore_backward(const uint8_t* codes, const void
     int sms = 0;
     cudaError_t e = q4_sms(&sms);
     if (e != cudaSuccess) return q4_done(e, 0, "4-bit rescore backward kernel");
+    // About 256 threads: 1024 x 100 of 768 26.5 us, with 128 37.5, with 512 31.5 (rows of 128 would rather have 128: 4096 x 100 22 instead of 33).
+    // Clusters while the queries do not fill the GPU and a team has 8 candidates left: 1 x 200 of 768 4.6 us, without 12.1; 16 x 500 of 1024
+    // 8.6 and 33.0.
     const int per_row = d / 16, teams = per_row >= 256 ? 1 : 256 / per_row, threads = (teams * per_row + 31) / 32 * 32;  // at most 512
     int cluster_log2 = 0;
     while ((1 << cluster_log2) < Q4B_MAX_CLUSTER && (int64_t)nq << cluster_log2 < 2 * sms && k >= (int64_t)(8 * teams) << cluster_log2) ++cluster_log2;
