@@ -100,12 +100,10 @@ __global__ void __launch_bounds__(BALANCE_THREADS) balance_clear_kernel(int32_t*
 
 // The smallest count, where the word that 1 / T goes to in the end holds it (volatile: read once, before the last CTA overwrites it)
 __device__ __forceinline__ int balance_kept(const BalanceTotals* totals) { return __float_as_int(*const_cast<const volatile float*>(&totals->per_slot)); }
-// The smallest of all counts, by a CTA.  Where there are fewer slots than lists it is 0 (looked at where that saves reading many counts:
-// the slots would be waited for), and a thread that has met a 0 is done.
+// The smallest of all counts, by a CTA.  A thread that has met a 0 is done.
 template <int THREADS>
-__device__ __forceinline__ int balance_least(const int32_t* counts, int nlist, uint32_t T) {
+__device__ __forceinline__ int balance_least(const int32_t* counts, int nlist) {
     __shared__ int least;
-    if (nlist > BALANCE_SHARED_LISTS && T < (uint32_t)nlist) return 0;
     if (threadIdx.x == 0) least = 0x7fffffff;
     __syncthreads();
     int base = 0x7fffffff;
@@ -124,12 +122,15 @@ __device__ __forceinline__ int balance_least(const int32_t* counts, int nlist, u
     return least;
 }
 
+// How the CTAs of long rows come by the smallest count: it is 0 where there are fewer slots than lists, which the host knows
+enum BalanceLeast { BALANCE_LEAST_0, BALANCE_LEAST_OWN, BALANCE_LEAST_KEPT };
+
 // SHARED: count in shared memory.  Up to BALANCE_OWN_LEAST counts, which 128 threads read in one go, the rows' CTAs find the smallest
 // themselves (0.8 us at 1021 rows of 4096 lists, 2.3 by the last CTA here); of more the last CTA here does (2.2 us at 4096 rows of
 // 8192 lists, 4.9 by the rows' CTAs).
 template <bool SHARED>
 __global__ void __launch_bounds__(BALANCE_COUNT_THREADS) balance_count_kernel(const int32_t* __restrict__ lists, const uint8_t* __restrict__ valid, int nq,
-                                                                              int nprobe, int nlist, int32_t* __restrict__ counts, BalanceTotals* __restrict__ totals) {
+                                                                              int nprobe, int nlist, bool find_least, int32_t* __restrict__ counts, BalanceTotals* __restrict__ totals) {
     extern __shared__ int32_t here[];
     const int tid = threadIdx.x;
     if (SHARED) {
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(BALANCE_COUNT_THREADS) balance_count_kernel(co
     if (SHARED)
         for (int l = tid; l < nlist; l += BALANCE_COUNT_THREADS)
             if (here[l]) atomicAdd(&counts[l], here[l]);
-    if (nlist <= BALANCE_OWN_LEAST) return;
+    if (!find_least) return;
     // the word of 1 / T counts the CTAs that are done, and holds the smallest count from then on until the rows are done
     __shared__ bool last;
     __threadfence();
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(BALANCE_COUNT_THREADS) balance_count_kernel(co
     __syncthreads();
     if (!last) return;
     __threadfence();
-    const int base = balance_least<BALANCE_COUNT_THREADS>(counts, nlist, __ldcg(&totals->slots));
+    const int base = balance_least<BALANCE_COUNT_THREADS>(counts, nlist);
     if (tid == 0) totals->per_slot = __int_as_float(base);
 }
 
@@ -415,7 +416,7 @@ __global__ void __launch_bounds__(BALANCE_THREADS) balance_short_rows_kernel(con
 // them (WHOLE: rows and counts of whole 16-byte pieces), or are at least met again in L1.
 template <bool BF16, int ROWS, bool WHOLE, int THREADS>
 __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balance_rows_kernel(const void* __restrict__ logits, int nq, int nlist, float a, const uint8_t* __restrict__ valid,
-                                                               const int32_t* __restrict__ counts, bool has_base, BalanceTotals* __restrict__ totals,
+                                                               const int32_t* __restrict__ counts, int how_least, BalanceTotals* __restrict__ totals,
                                                                uint32_t* __restrict__ ticket, float4* __restrict__ stats, float* __restrict__ loss) {
     using P = LogitPiece<BF16>;
     __shared__ BalanceSums part[THREADS / 32][ROWS];
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
     const int q0 = blockIdx.x * ROWS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t T = totals->slots;
     int base = 0;
-    if (has_base) base = balance_kept(totals);
+    if (how_least == BALANCE_LEAST_KEPT) base = balance_kept(totals);
     BalanceSums S[ROWS];
     bool counted[ROWS];
 #pragma unroll
@@ -434,10 +435,10 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
         counted[r] = q0 + r < nq && (!valid || valid[q0 + r]);
     }
     if (ROWS == 1) {
-        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
+        if (how_least == BALANCE_LEAST_OWN) base = balance_least<THREADS>(counts, nlist);
         if (counted[0]) balance_sweep<BF16>(S[0], logits, (size_t)q0 * nlist, nlist, a, counts, base, tid, THREADS);
     } else if (!WHOLE) {
-        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
+        if (how_least == BALANCE_LEAST_OWN) base = balance_least<THREADS>(counts, nlist);
         int head[ROWS], pieces[ROWS], most = 0;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -476,7 +477,7 @@ __global__ void __launch_bounds__(THREADS, ROWS > 1 ? 7 : 1024 / THREADS) balanc
                 if (counted[r] && l < nlist) next[r] = P::load(logits, (size_t)(q0 + r) * nlist + l);
         };
         fetch(tid * P::UNIT);
-        if (!has_base) base = balance_least<THREADS>(counts, nlist, T);
+        if (how_least == BALANCE_LEAST_OWN) base = balance_least<THREADS>(counts, nlist);
         for (int l = tid * P::UNIT; l < nlist; l += THREADS * P::UNIT) {
             uint4 w[ROWS];
 #pragma unroll
@@ -739,7 +740,7 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
     const int range = (int)parts_of(nlist, ranges);
     cudaError_t e;
     const bool ranges_do = slots <= BALANCE_RANGE_SLOTS && range <= BALANCE_SHARED_LISTS;
-    const bool has_base = !ranges_do && nlist > BALANCE_OWN_LEAST;  // the smallest count is known before the rows
+    const int how_least = slots < nlist ? BALANCE_LEAST_0 : ranges_do || nlist <= BALANCE_OWN_LEAST ? BALANCE_LEAST_OWN : BALANCE_LEAST_KEPT;
     if (ranges_do) {
         e = launch_overlapped(balance_count_ranges_kernel, dim3((unsigned)parts_of(nlist, range)), dim3(BALANCE_RANGE_THREADS), (size_t)range * 4, s, lists, valid,
                               nq, nprobe, nlist, range, out_counts, totals, ticket);
@@ -752,7 +753,7 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
         if (e == cudaSuccess && slots) {
             const int64_t ctas = parts_of(slots, 8 * BALANCE_COUNT_THREADS);
             e = launch_overlapped(shared ? balance_count_kernel<true> : balance_count_kernel<false>, dim3((unsigned)(ctas < 4096 ? ctas : 4096)), dim3(BALANCE_COUNT_THREADS),
-                                  shared ? (size_t)nlist * 4 : 0, s, lists, valid, nq, nprobe, nlist, out_counts, totals);
+                                  shared ? (size_t)nlist * 4 : 0, s, lists, valid, nq, nprobe, nlist, how_least == BALANCE_LEAST_KEPT, out_counts, totals);
             ++launches;
         }
     }
@@ -762,7 +763,7 @@ extern "C" rago_status rago_list_balance(const void* logits, rago_dtype dtype, i
         auto rows = [&](auto bf16) {
             constexpr bool B = decltype(bf16)::value;
             auto launch = [&](auto kernel, int per_cta, int threads) {
-                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts, has_base,
+                return launch_overlapped(kernel, dim3((unsigned)parts_of(nq, per_cta)), dim3((unsigned)threads), 0, s, logits, nq, nlist, a, valid, out_counts, how_least,
                                          totals, ticket, stats, out_loss);
             };
             auto launch_short = [&](auto kernel, int per_cta) {
