@@ -453,7 +453,9 @@ rago_status rago_policy_loss_backward(const void* scores, const void* ref_scores
  * (a search's time is the bytes of the lists it probes).  With T the slots counted, n the rows counted, p = softmax(scale * logits) of a row,
  *     counts_l = slots of counted rows that name list l,   f_l = counts_l / T
  *     loss     = nlist / n * sum_rows sum_l f_l p_l        (1 for even lists or an even p)
- *   logits     dev [nq][nlist], RAGO_F32 or RAGO_BF16: the coarse scores; -infinity after scaling is p = 0.  A row without a finite
+ *   logits     dev [nq][nlist], RAGO_F32 or RAGO_BF16: the coarse scores of all lists, as the program that trains the centroids computes
+ *              them (an index's are borrowed and stay as they are from load to free; trained ones are loaded anew); -infinity after
+ *              scaling is p = 0.  A row without a finite
  *              one, and all of its slots, count in n, T and counts, and add nothing to the loss
  *   scale      finite, at least 1e-36 in magnitude: 1 / temperature, negative for distances
  *   lists      dev int32 [nq][nprobe] as rago_search_probes leaves them; a number outside 0 .. nlist - 1 is not counted

@@ -42,9 +42,10 @@ __device__ __forceinline__ float load_f(const void* base, size_t i) {
 // across its tiles and never meets the other warps of its CTA, which share the queries in shared memory only.  The order of a row's
 // numbers is permuted alike in rows and queries: thread t of a quad takes word t of every 16 bytes, whatever the group.
 //
-// Measured: 10 M rows of 1024 (groups of 128) for 8 bf16 queries 1 043 us = 5.4 TB/s, bound by unpacking (2.3 instructions a number and
-// lane, 67% of the issue slots); 100 000 rows of 768 for one fp32 query 15 us, 4 of them before the first product; 1 000 003 rows of 768
-// (groups of 32) for 37 queries 255 us, where each group's 80 sums a lane are scaled between the matrix instructions.
+// Measured: 10 M rows of 1024 (groups of 128) for 8 bf16 queries 985 to 1 050 us in twenty calls at 1 965 MHz (5.3 to 5.7 TB/s), 1 170 to 1 240 in
+// a stream of thousands, where 1 kW holds the clock at 1 640 to 1 560 MHz; bound by unpacking (2.4 instructions a number and lane, 70% of
+// the issue slots).  100 000 rows of 768 for one fp32 query 15 us, 4 of them before the first product; 1 000 003 rows of 768 (groups of 32)
+// for 37 queries 228 us, where each group's 80 sums a lane are scaled between the matrix instructions.
 constexpr int Q4S_ROWS = 32, Q4S_STRIDE = 80;  // 64 bytes of a row a stage, spaced 20 words: the 8 rows of a fragment meet no bank twice
 constexpr int Q4S_STAGE = Q4S_ROWS * Q4S_STRIDE;
 // Most tiles of columns (times parts) for which warps may share a tile of rows.  (1000 rows of 768 for one query 4.1 us, not shared 4.9; three and four
@@ -571,7 +572,7 @@ __global__ void __launch_bounds__(Q4R_WARPS * 32) q4_rescore_kernel(const Q4Rows
 // would cancel where candidates are near, 3e-5 of the gradient for queries 0.01 |query| away.  A thread owns 16 numbers, 8 bytes of a row; teams of
 // d / 16 threads take the candidates in turn, their sums meet in shared memory, where the query lies too.  With few queries a cluster of CTAs shares the candidates
 // of one, and adds its sums up through distributed shared memory.  Missing candidates are left out when ids and gradients are staged, so
-// nothing of theirs is looked at.  Measured: 1024 queries' 100 candidates of 768 numbers 30 us, which is latency: ids, rows, sums of the
+// nothing of theirs is looked at.  Measured: 1024 queries' 100 candidates of 768 numbers 28 us (distance; 22 for inner products), which is latency: ids, rows, sums of the
 // teams, one after the other, in a CTA that lives for 20 rows a team.
 constexpr int Q4B_THREADS = 512, Q4B_STAGE = 512, Q4B_MAX_CLUSTER = 8;  // candidates staged at a time
 
