@@ -34,7 +34,9 @@ __device__ __forceinline__ float load_f(const void* base, size_t i) {
 // the products.
 // Queries go in as fp16 after a power of two per query that brings its largest number to 2^14 .. 2^15 (taken off the sums again):
 // a bf16 number fits as it is, an fp32 number is cut into two parts, hi = fp16(x) and fp16(x - hi), 23 of its 24 bits: off by at
-// most 2^-23 of itself, or by 2^-39 of the query's largest number where that is more.  The parts'
+// most 2^-23 of itself, or by 2^-39 of the query's largest number where that is more.  (A third part for the last bit would be half as many
+// matrix instructions again; that bit lies below the rounding of the fp32 sums: 7e-8 of the scores' size against 64 bits, plain fp32
+// sums 1.3e-7.)  The parts'
 // products add up in the same fp32 accumulators; up to four fp32 queries put their parts side by side into the eight columns, so that
 // one instruction does for all of them.  The sum over a group is multiplied by the row's scale and added to the row's total.
 //
